@@ -136,6 +136,19 @@ typedef struct swarm_medoid_index {
                                     /* of the cluster scores                                                           */
 } swarm_medoid_index;
 
+/* Drafted tokens of a batch of requests: a tree per request whose tokens follow the cached context.  Device pointers.
+ * Row t of request b exists iff t < n_draft[b]; what stands in q, k and v behind may hold anything. */
+typedef struct swarm_tree {
+  const void* q;           /* bf16 [B][T][Hq][d]                                                             */
+  const void* k;           /* bf16 [B][T][Hkv][d] keys and values of the drafted tokens (not in the pool)    */
+  const void* v;           /* bf16 [B][T][Hkv][d]                                                            */
+  const int32_t* n_draft;  /* [B] drafted tokens of each request, 0..T                                       */
+  const uint32_t* mask;    /* [B][T][ceil(T/32)] bit j % 32 of word j / 32 of row t: token t attends drafted */
+                           /* token j (itself included only if its bit is set).  NULL: a chain, j <= t       */
+  int32_t max_draft;       /* T                                                                              */
+  int32_t reserved;        /* must be 0                                                                      */
+} swarm_tree;
+
 /* Lifetime.  swarm_create validates the shape and allocates only host memory.
  * The CUDA device current at creation must stay current for every later call with this ctx. */
 int32_t swarm_create(const swarm_shape* shape, swarm_ctx** out_ctx);
@@ -400,6 +413,24 @@ int64_t swarm_build_clusters_workspace_bytes(int32_t n_entries);
 int32_t swarm_build_clusters(const float* dist, int32_t n_entries, float tau, void* workspace, int64_t workspace_bytes,
                              int32_t* density, int32_t* cluster_ptr, int32_t* cluster_members, int64_t members_cap,
                              int32_t* medoid, int32_t* n_clusters, int32_t* dev_status, void* stream);
+
+/* Attention of drafted tokens over the cache (verification of speculative decoding; with max_draft = 1 the attention of a
+ * single new token over its whole context, with mask = NULL a chunk of a prompt).  For t < n_draft[b]
+ *   out[b][t][h] = softmax_j(q[b][t][h] . K_j / sqrt(d)) V_j,  lse[b][t][h] = log sum_j exp(q[b][t][h] . K_j / sqrt(d))
+ * over the tokens j of the request's context (ctx_len[b] of them, here 0 is allowed) and its drafted tokens that
+ * the mask shows row t.  sel / n_sel (both or neither): only the context pages selected for head h, as swarm_select
+ * writes them (a page listed twice counts once; ids outside the request set SWARM_DEV_BAD_PAGE and are skipped); NULL:
+ * all pages.  A row that sees no token gives out = 0, lse = -inf.  Rows t >= n_draft[b] of out and lse are left as
+ * they were.  out is bf16 [B][T][Hq][d] (the weights enter the product with V as bf16), lse f32 [B][T][Hq].
+ * A context length that does not fit the request's pages sets SWARM_DEV_BAD_LENGTH and the request's rows are left as they
+ * were; n_draft outside 0..T sets it too and is clamped.
+ * Reads inputs->kv_pool, page_base, ctx_len.  workspace: swarm_tree_attn_workspace_bytes(shape, T) bytes of device
+ * memory (256-byte aligned, contents irrelevant), used by one call at a time; < 0: minus an error code.
+ * SWARM_ERR_UNSUPPORTED: n_pool_pages >= 2^31; with a selection, more than 32 query heads per KV head or more than 655360
+ * pages per request. */
+int64_t swarm_tree_attn_workspace_bytes(const swarm_shape* shape, int32_t max_draft);
+int32_t swarm_tree_attn(swarm_ctx* ctx, const swarm_inputs* inputs, const swarm_tree* tree, const int32_t* sel,
+                        const int32_t* n_sel, void* workspace, int64_t workspace_bytes, void* out, float* lse, void* stream);
 
 /* End-to-end convenience for callers holding the per-step data in HOST memory (pinned memory
  * recommended): copies q_host (bf16 [B][Hq][d]) into the ctx's staging area, runs swarm_step with

@@ -32,6 +32,7 @@ EXPORTS = (
     "swarm_build_clusters_workspace_bytes", "swarm_build_clusters",
     "swarm_cache_admit_workspace_bytes", "swarm_cache_admit",
     "swarm_step_begin", "swarm_step_end", "swarm_cluster_flags",
+    "swarm_tree_attn_workspace_bytes", "swarm_tree_attn",
 )
 
 
@@ -81,6 +82,7 @@ def load_library() -> ctypes.CDLL:
         lib.swarm_workspace_bytes.restype = ctypes.c_int64
         lib.swarm_build_clusters_workspace_bytes.restype = ctypes.c_int64
         lib.swarm_cache_admit_workspace_bytes.restype = ctypes.c_int64
+        lib.swarm_tree_attn_workspace_bytes.restype = ctypes.c_int64
         v, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
         lib.swarm_build_clusters.argtypes = [v, i32, ctypes.c_float, v, i64, v, v, v, i64, v, v, v, v]
         _lib = lib
@@ -416,6 +418,54 @@ def _step_host_fn():
     if _STEP_HOST_FN is None:
         _STEP_HOST_FN = load_library().swarm_step_host
     return _STEP_HOST_FN
+
+
+class swarm_tree(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "n_draft", "mask")] + \
+               [("max_draft", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+def _expect(t: torch.Tensor, name: str, dtype, shape) -> None:
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+
+
+def make_tree(*, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_draft: torch.Tensor,
+              mask: Optional[torch.Tensor] = None) -> swarm_tree:
+    """Drafted tokens: q [B, T, Hq, 128], k and v [B, T, Hkv, 128] (bf16), n_draft int32 [B], mask int32 [B, T, ceil(T/32)]
+    (bit j of a row: it attends drafted token j) or None for a chain.  The caller keeps the tensors alive while the struct
+    is in use."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k must have four dimensions: request, drafted token, head, coordinate")
+    batch, T = q.shape[:2]
+    _expect(q, "q", torch.bfloat16, (batch, T, q.shape[2], 128))
+    _expect(k, "k", torch.bfloat16, (batch, T, k.shape[2], 128))
+    _expect(v, "v", torch.bfloat16, k.shape)
+    _expect(n_draft, "n_draft", torch.int32, (batch,))
+    if mask is not None:
+        _expect(mask, "mask", torch.int32, (batch, T, -(-T // 32)))
+    return swarm_tree(_ptr(q, "q"), _ptr(k, "k"), _ptr(v, "v"), _ptr(n_draft, "n_draft"), _ptr(mask, "mask"), T, 0)
+
+
+def swarm_tree_attn_workspace_bytes(shape: swarm_shape, max_draft: int) -> int:
+    n = int(load_library().swarm_tree_attn_workspace_bytes(ctypes.byref(shape), ctypes.c_int32(max_draft)))
+    if n < 0:
+        raise SwarmError(-n, "swarm_tree_attn_workspace_bytes")
+    return n
+
+
+def swarm_tree_attn(ctx, inputs: swarm_inputs, tree: swarm_tree, sel: Optional[torch.Tensor], n_sel: Optional[torch.Tensor],
+                    workspace: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, stream=None) -> None:
+    """Attention of the drafted tokens over the context (all pages, or those selected per head) and over one another;
+    out bf16 [B, T, Hq, 128], lse float32 [B, T, Hq]."""
+    if out.dtype != torch.bfloat16 or lse.dtype != torch.float32:
+        raise ValueError("out must be bfloat16 and lse float32")
+    rc = load_library().swarm_tree_attn(ctx, ctypes.byref(inputs), ctypes.byref(tree), _ptr(sel, "sel"), _ptr(n_sel, "n_sel"),
+                                        _ptr(workspace, "workspace"),
+                                        ctypes.c_int64(workspace.numel() * workspace.element_size()), _ptr(out, "out"),
+                                        _ptr(lse, "lse"), _stream(stream))
+    if rc != OK:
+        _check(rc, "swarm_tree_attn", ctx)
 
 
 def swarm_device_status(ctx, stream=None) -> int:

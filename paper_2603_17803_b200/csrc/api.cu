@@ -72,6 +72,16 @@ int32_t check_shape(const swarm_shape* s) {
   return SWARM_OK;
 }
 
+Geometry geometry_of(const swarm_shape& s) {
+  Geometry g;
+  g.B = s.batch; g.Hq = s.n_q_heads; g.Hkv = s.n_kv_heads; g.g = g.Hq / g.Hkv;
+  g.S = s.page_size; g.k = s.top_k; g.D = s.n_queues; g.Pmax = s.max_pages_per_req;
+  g.Cmax = s.max_clusters_total; g.flags = s.flags; g.n_pool_pages = s.n_pool_pages;
+  g.W = s.local_window_pages;
+  g.scorer = SWARM_SCORER_AUTO;
+  return g;
+}
+
 WorkspaceLayout make_layout(const swarm_shape& s) {
   WorkspaceLayout l;
   const int64_t bh = (int64_t)s.batch * s.n_q_heads;
@@ -271,12 +281,7 @@ int32_t swarm_create(const swarm_shape* shape, swarm_ctx** out_ctx) {
   swarm_ctx* ctx = new (std::nothrow) swarm_ctx();
   if (ctx == nullptr) return SWARM_ERR_INVALID_ARG;
   ctx->shape = *shape;
-  Geometry& g = ctx->geo;
-  g.B = shape->batch; g.Hq = shape->n_q_heads; g.Hkv = shape->n_kv_heads; g.g = g.Hq / g.Hkv;
-  g.S = shape->page_size; g.k = shape->top_k; g.D = shape->n_queues; g.Pmax = shape->max_pages_per_req;
-  g.Cmax = shape->max_clusters_total; g.flags = shape->flags; g.n_pool_pages = shape->n_pool_pages;
-  g.W = shape->local_window_pages;
-  g.scorer = SWARM_SCORER_AUTO;
+  ctx->geo = geometry_of(*shape);
   ctx->lay = make_layout(*shape);
   ctx->ws = nullptr;
   ctx->ws_bytes = 0;
@@ -314,6 +319,7 @@ int32_t swarm_create(const swarm_shape* shape, swarm_ctx** out_ctx) {
   if (e == cudaSuccess) e = configure_resolve();
   if (e == cudaSuccess) e = configure_attention();
   if (e == cudaSuccess) e = configure_medoid();
+  if (e == cudaSuccess) e = configure_tree();
   if (e != cudaSuccess) {
     if (ctx->done_h != nullptr) cudaFreeHost(ctx->done_h);
     delete ctx;
@@ -858,6 +864,44 @@ int32_t swarm_step_medoid(swarm_ctx* ctx, const swarm_inputs* in, const swarm_me
     rs.has_cache = false;
   }
   SWARM_TRY(launch_attention(ctx->geo, a, status, st, /*overlap=*/true, &rs));
+  return SWARM_OK;
+}
+
+int64_t swarm_tree_attn_workspace_bytes(const swarm_shape* shape, int32_t max_draft) {
+  const int32_t rc = check_shape(shape);
+  if (rc != SWARM_OK) return -(int64_t)rc;
+  if (max_draft < 1) return -(int64_t)SWARM_ERR_INVALID_ARG;
+  const Geometry g = geometry_of(*shape);
+  if (!tree_supported(g, max_draft, false)) return -(int64_t)SWARM_ERR_UNSUPPORTED;
+  return tree_attn_workspace_bytes(g, max_draft);
+}
+
+int32_t swarm_tree_attn(swarm_ctx* ctx, const swarm_inputs* in, const swarm_tree* tree, const int32_t* sel, const int32_t* n_sel,
+                        void* workspace, int64_t workspace_bytes, void* out, float* lse, void* stream) {
+  SWARM_RANGE("swarm_tree_attn");
+  int32_t rc = need_ws(ctx);
+  if (rc != SWARM_OK) return rc;
+  if (!pool_inputs_ok(in) || tree == nullptr || bad(tree->q) || bad(tree->k) || bad(tree->v) || bad(tree->n_draft) ||
+      !aligned16(tree->mask) || tree->max_draft < 1 || tree->reserved != 0 || (sel == nullptr) != (n_sel == nullptr) ||
+      !aligned16(sel) || !aligned16(n_sel) || workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bad(out) || bad(lse))
+    return SWARM_ERR_INVALID_ARG;
+  if (!tree_supported(ctx->geo, tree->max_draft, sel != nullptr)) return SWARM_ERR_UNSUPPORTED;
+  if (workspace_bytes < tree_attn_workspace_bytes(ctx->geo, tree->max_draft)) return SWARM_ERR_WORKSPACE_TOO_SMALL;
+  TreeCall c{};
+  c.q = static_cast<const uint16_t*>(tree->q);
+  c.k = static_cast<const uint16_t*>(tree->k);
+  c.v = static_cast<const uint16_t*>(tree->v);
+  c.n_draft = tree->n_draft;
+  c.mask = tree->mask;
+  c.T = tree->max_draft;
+  c.kv_pool = static_cast<const uint16_t*>(in->kv_pool);
+  c.page_base = in->page_base;
+  c.ctx_len = in->ctx_len;
+  c.sel = sel;
+  c.n_sel = n_sel;
+  c.out = static_cast<uint16_t*>(out);
+  c.lse = lse;
+  SWARM_TRY(launch_tree_attn(ctx->geo, c, workspace, ws_ptr<uint32_t>(ctx, ctx->lay.status), static_cast<cudaStream_t>(stream)));
   return SWARM_OK;
 }
 

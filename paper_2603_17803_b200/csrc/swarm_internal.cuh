@@ -296,6 +296,28 @@ cudaError_t launch_medoid_rows(const Geometry& geo, const uint16_t* ksum, const 
 cudaError_t launch_expand_clusters(const ExpandArgs& ex, const Geometry& geo, int k_c, const int32_t* sel_c, const int32_t* n_sel_c, uint32_t* status,
                                    cudaStream_t st, bool overlap);
 
+// Attention of drafted tokens over the cache: see tree.cu.
+constexpr int kMaxTreeMapBytes = 160 * 1024;              // largest page bitmap (with its counts) of a unit in shared memory
+struct TreeCall {
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  const int32_t* n_draft;
+  const uint32_t* mask;
+  int T;
+  const uint16_t* kv_pool;
+  const int64_t* page_base;
+  const int32_t* ctx_len;
+  const int32_t* sel;
+  const int32_t* n_sel;
+  uint16_t* out;
+  float* lse;
+};
+bool tree_supported(const Geometry& geo, int T, bool selected);
+long long tree_attn_workspace_bytes(const Geometry& geo, int T);
+cudaError_t configure_tree();
+cudaError_t launch_tree_attn(const Geometry& geo, const TreeCall& c, void* workspace, uint32_t* status, cudaStream_t st);
+
 // Algorithm 1 (offline co-activation clustering): see cluster.cu.
 long long build_clusters_workspace_bytes(int n);
 cudaError_t launch_build_clusters(const float* dist, int n, float tau, void* workspace, int32_t* rho, int32_t* ptr,

@@ -1,0 +1,1013 @@
+// Attention of a tree of drafted tokens over the paged cache (swarm_tree_attn).
+//
+// Row (t, h) of request b, t < n_draft[b]:  s_j = q . k_j / sqrt(d) over the context's tokens (of all pages, or of the
+// pages selected for head h) and over the drafted tokens j that the mask shows row t;
+//   out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  lse = m + log sum_j exp(s_j - m),  in one pass over K and V.
+// The g query heads of a KV head and the drafted tokens of a request see the same keys: they are the up to 256 rows of one
+// matrix product with every tile of 128 tokens, so K and V are read once for all of them.
+//
+//   warps 0-3, 4-7   two softmax streams, a thread per row of 128 (tcgen05.ld: lane = row)
+//   warp 8           copies: K and V tiles of 32 KB by TMA into a ring, 128-byte swizzle
+//   warp 9           matrix products: S = Q K^T (operands in shared memory), O += P V (P from tensor memory)
+// Tensor memory: S0, S1 (128 columns each; P, in bf16, takes the place of S), O0, O1.  While one stream is in its softmax
+// the tensor core works for the other.  Up to 128 rows: the streams take alternate tiles of the same rows, and their
+// sums are joined at the end through tensor memory; beyond, each has 128 rows of its own and both use every tile.
+//
+// The tiles of all (request, KV head) units form one list that is cut evenly over the CTAs, whatever the lengths
+// are; a unit that is cut leaves partial (m, l, O) per CTA, joined by a second kernel with a warp per row.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <algorithm>
+
+#include "swarm_internal.cuh"
+
+namespace swarm {
+namespace {
+
+constexpr int kTile = 128;                                 // tokens of a tile, rows of a stream
+constexpr int kTileBytes = kTile * kHeadDim * 2;           // K or V of a tile: two halves of 64 coordinates
+constexpr int kHalfBytes = kTileBytes / 2;
+constexpr int kThreads = 320;
+constexpr int kSegs = 32;                                  // segments of a CTA listed at a time
+constexpr int kMaxTreeCtas = 148;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr unsigned kWaitLimit = 1u << 22;                  // polls of a try_wait that itself blocks briefly
+// The running maximum is raised only when a tile exceeds it by more than 2^8: until then the exponentials stay below
+// 2^8 * 128 terms, far from any limit of fp32 or bf16, and O needs no rescaling (the final division cancels the reference).
+constexpr float kMaxSlack = 8.f;
+
+struct Seg {                                               // tiles [t0, t1) of one unit
+  int b, kv;
+  int t0, t1;
+  int ctx_tiles, ctx_tokens;
+  int nd;                                                  // drafted tokens
+  int last;                                                // t1 ends the unit
+};
+
+constexpr int kSegIntsPerRow = 8;
+static_assert(sizeof(Seg) == kSegIntsPerRow * 4, "listed as words");
+
+template <bool kWide>
+struct Layout {
+  static constexpr int kQTiles = kWide ? 2 : 1;
+  static constexpr int kSlots = kWide ? 4 : 5;
+  static constexpr int kRows = kQTiles * kTile;
+  static constexpr int kRing = kQTiles * kTileBytes;
+  static constexpr int kBars = kRing + kSlots * kTileBytes;
+  static constexpr int kList = kBars + 256;
+  static constexpr int kMl = kList + kSegs * (int)sizeof(Seg);
+  static constexpr int kScan = kMl + 2 * kTile * 8;
+  static constexpr int kBytes = kScan + 256;
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint64_t* bar, unsigned count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count));
+}
+__device__ __forceinline__ void bar_expect(uint64_t* bar, unsigned bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t* bar, unsigned parity) {
+  unsigned ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_addr(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// Bounded wait of a whole warp.  When it runs out, `stop` tells the other warps of the CTA, whose waits then end as well;
+// the lanes agree on the answer.
+__device__ __forceinline__ bool bar_wait(uint64_t* bar, unsigned parity, volatile int* stop) {
+  bool there = false;
+  for (unsigned polls = 0; polls < kWaitLimit; ++polls) {
+    there = bar_try(bar, parity);
+    if (there || *stop != 0) break;
+  }
+  if (!there) *stop = 1;
+  return __all_sync(0xFFFFFFFFu, there);
+}
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int c1, int c2, int c3, int c4, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+      "l"(map), "r"(0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(smem_addr(bar))
+      : "memory");
+}
+
+// ---- tensor memory and tcgen05 ------------------------------------------------------------------------------------------
+__device__ __forceinline__ void tmem_ld32(uint32_t (&r)[32], uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+      "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+      "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+// Shared-memory operand with the 128-byte swizzle: `lead` and `stride` in bytes.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead, uint32_t stride) {
+  return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(stride >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// bf16 x bf16 -> fp32, 128 x 128; `transposed`: the second operand is stored with its rows along the products' sum
+__host__ __device__ constexpr uint32_t mma_shape(bool transposed) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (transposed ? 1u << 16 : 0u) | ((uint32_t)(kTile / 8) << 17) | ((uint32_t)(kTile / 16) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ float exp2_fast(float x) {      // 2^x, relative error about 2^-22; 0 for x = -inf
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+struct TreeArgs {
+  Geometry geo;
+  const uint16_t* q;
+  const int64_t* page_base;
+  const int32_t* ctx_len;
+  const int32_t* n_draft;
+  const uint32_t* mask;       // [B][T][words] or null: a chain
+  const int2* list;           // selected pages: [B*Hkv][list_cap] {page, heads}; null: all pages
+  const int32_t* list_tokens; // [B*Hkv] context tokens among them
+  int list_cap;
+  int T, words, row_blocks, chunks;
+  float* part_o;              // [CTA][2][rows][128]
+  float2* part_ml;            // [CTA][2][rows]
+  int32_t* unit_first;        // [B*Hkv] 2 * chunk + place of the unit's first partial
+  int32_t* unit_last;         // [B*Hkv] its last chunk
+  uint16_t* out;
+  float* lse;
+  uint32_t* status;
+};
+
+// Context tokens (those of the selected pages, if there is a selection) and drafted tokens of a unit; no drafted
+// tokens where the request's length does not fit its pages.
+__device__ __forceinline__ void unit_lengths(const TreeArgs& a, int u, int& ctx, int& nd, bool& bad) {
+  const int b = u / a.geo.Hkv;
+  const int len = a.ctx_len[b];
+  const long long owned = a.page_base[b + 1] - a.page_base[b];
+  nd = a.n_draft[b];
+  bad = nd < 0 || nd > a.T;
+  nd = max(0, min(nd, a.T));
+  if (len < 0 || pages_of(len, a.geo.S) > owned) {
+    bad = true;
+    nd = 0;
+  }
+  ctx = a.list != nullptr ? a.list_tokens[u] : len;
+}
+__device__ __forceinline__ int tiles_of(int ctx, int nd) {
+  return nd == 0 ? 0 : (ctx + kTile - 1) / kTile + (nd + kTile - 1) / kTile;
+}
+
+template <bool kWide>
+__global__ void __launch_bounds__(kThreads, 1)
+tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_constant__ CUtensorMap pool_page,
+                 const __grid_constant__ CUtensorMap draft_k, const __grid_constant__ CUtensorMap draft_v, const TreeArgs a) {
+  using L = Layout<kWide>;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBars);
+  uint64_t *full = bars, *empty = bars + 6, *s_full = bars + 12, *p_full = bars + 14, *q_full = bars + 16, *joined = bars + 17,
+           *drained = bars + 18;
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + 20);
+  volatile int* stop = reinterpret_cast<volatile int*>(bars + 21);
+  int* n_segs = reinterpret_cast<int*>(bars + 22);
+  Seg* list = reinterpret_cast<Seg*>(smem + L::kList);
+  float2* ml = reinterpret_cast<float2*>(smem + L::kMl);     // [2][128] of the two streams
+  long long* scan = reinterpret_cast<long long*>(smem + L::kScan);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rb = blockIdx.x % a.row_blocks, chunk = blockIdx.x / a.row_blocks;
+  const int g = a.geo.g, Hkv = a.geo.Hkv, S = a.geo.S;
+  const int units = a.geo.B * Hkv;
+
+  if (tid == 0) {
+    for (int i = 0; i < L::kSlots; ++i) { bar_init(full + i, 1); bar_init(empty + i, 1); }
+    for (int i = 0; i < 2; ++i) { bar_init(s_full + i, 1); bar_init(p_full + i, 4); }
+    bar_init(q_full, 8);
+    bar_init(joined, 8);
+    bar_init(drained, 1);
+    *stop = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(tmem_at)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    tc_fence_before();
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+
+  // ---- this CTA's share of all tiles: the list of units is summed by the whole CTA, the unit of its first tile found
+  const int per = (units + kThreads - 1) / kThreads;
+  const int u_lo = min(units, tid * per), u_hi = min(units, u_lo + per);
+  long long mine = 0;
+  for (int u = u_lo; u < u_hi; ++u) {
+    int ctx, nd;
+    bool bad;
+    unit_lengths(a, u, ctx, nd, bad);
+    if (bad && blockIdx.x == 0 && u % Hkv == 0) atomicOr(a.status, SWARM_DEV_BAD_LENGTH);
+    mine += tiles_of(ctx, nd);
+  }
+  long long incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 31) scan[warp] = incl;
+  __syncthreads();
+  tc_fence_after();
+  long long before = incl - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) before += scan[w];
+    total += scan[w];
+  }
+  const long long w0 = total * chunk / a.chunks, w1 = total * (chunk + 1) / a.chunks;
+  if (w0 < w1 && before <= w0 && w0 < before + mine) {       // one thread: its units hold the first tile
+    int u = u_lo;
+    long long at = before;
+    for (; u < u_hi; ++u) {
+      int ctx, nd;
+      bool bad;
+      unit_lengths(a, u, ctx, nd, bad);
+      const int n = tiles_of(ctx, nd);
+      if (at + n > w0) break;
+      at += n;
+    }
+    scan[12] = u;
+    scan[13] = at;
+  }
+  __syncthreads();
+  const uint32_t tmem = *tmem_at;
+
+  // state of the roles, carried from one list of segments to the next
+  int slot = 0;
+  unsigned ring_phase = 0u;                                  // parity of the current round through the ring
+  unsigned s_phase = 0u, p_phase = 0u, q_phase = 0u, j_phase = 0u;   // (p_phase: a bit per stream)
+  int issued = 0;                                            // copies started (producer)
+  bool ok = true;
+  bool first_list = true;
+  int u_next = w0 < w1 ? (int)scan[12] : units;
+  long long at_next = w0 < w1 ? scan[13] : 0;
+
+  while (u_next < units && at_next < w1) {
+    // ---- the next (up to 32) units with tiles in this CTA's share
+    __syncthreads();                                         // the previous list has been worked through
+    if (warp == 0) {
+      const int u = u_next + lane;
+      int ctx = 0, nd = 0, n = 0;
+      bool bad;
+      if (u < units) {
+        unit_lengths(a, u, ctx, nd, bad);
+        n = tiles_of(ctx, nd);
+      }
+      long long end = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xFFFFFFFFu, end, o);
+        if (lane >= o) end += v;
+      }
+      end += at_next;
+      const long long begin = end - n;
+      const bool here = n > 0 && begin < w1 && end > w0;
+      const unsigned all = __ballot_sync(0xFFFFFFFFu, here);
+      if (here) {
+        Seg s;
+        s.b = u / Hkv;
+        s.kv = u - s.b * Hkv;
+        s.t0 = (int)(max(w0, begin) - begin);
+        s.t1 = (int)(min(w1, end) - begin);
+        s.ctx_tiles = (ctx + kTile - 1) / kTile;
+        s.ctx_tokens = ctx;
+        s.nd = nd;
+        s.last = s.t1 == n;
+        list[__popc(all & ((1u << lane) - 1u))] = s;
+        if (rb == 0) {
+          if (s.t0 == 0) a.unit_first[u] = 2 * chunk + (begin == w0 ? 0 : 1);
+          if (s.last) a.unit_last[u] = chunk;
+        }
+      }
+      if (lane == 31) scan[14] = end;
+      if (lane == 0) *n_segs = __popc(all);
+    }
+    __syncthreads();
+    const int count = *n_segs;
+    u_next += 32;
+    at_next = scan[14];
+
+    if (warp == 8) {
+      // ---- copies, in the order the matrix products use them
+      auto load_tile = [&](const Seg& s, int t, int which) -> bool {   // which: 0 = K, 1 = V
+        if (issued >= L::kSlots && !bar_wait(empty + slot, ring_phase ^ 1u, stop)) return false;
+        const uint32_t dst = smem_addr(smem + L::kRing + slot * kTileBytes);
+        uint64_t* bar = full + slot;
+        if (t >= s.ctx_tiles) {                              // drafted tokens; rows behind the last are filled with zeros
+          if (lane == 0) {
+            bar_expect(bar, kTileBytes);
+            tma_load(dst, which == 0 ? &draft_k : &draft_v, (t - s.ctx_tiles) * kTile, 0, s.kv, s.b, bar);
+          }
+        } else if (a.list == nullptr) {
+          if (lane == 0) {
+            bar_expect(bar, kTileBytes);
+            tma_load(dst, &pool_tile, 0, (int)(a.page_base[s.b] + (long long)t * (kTile / S)), 0, s.kv * 2 + which, bar);
+          }
+        } else {                                             // the tile's pages one by one, a lane each
+          const int per_tile = kTile / S, pages = min(per_tile, (s.ctx_tokens + S - 1) / S - t * per_tile);
+          if (lane == 0) bar_expect(bar, (unsigned)(pages * S * kHeadDim * 2));
+          __syncwarp();
+          if (lane < pages) {
+            const int page = (int)a.page_base[s.b] + a.list[(long long)(s.b * Hkv + s.kv) * a.list_cap + t * per_tile + lane].x;
+            for (int h = 0; h < 2; ++h)
+              tma_load(dst + h * kHalfBytes + lane * S * 128, &pool_page, 0, page, h, s.kv * 2 + which, bar);
+          }
+        }
+        __syncwarp();
+        ++issued;
+        if (++slot == L::kSlots) { slot = 0; ring_phase ^= 1u; }
+        return true;
+      };
+      for (int i = 0; ok && i < count; ++i) {
+        const Seg s = list[i];
+        if (rb * L::kRows >= s.nd * g) continue;
+        const int n = s.t1 - s.t0;
+        if constexpr (kWide) {
+          ok = load_tile(s, s.t0, 0);
+          for (int t = 0; ok && t < n; ++t) {
+            ok = load_tile(s, s.t0 + t, 1);
+            if (ok && t + 1 < n) ok = load_tile(s, s.t0 + t + 1, 0);
+          }
+        } else {
+          ok = load_tile(s, s.t0, 0);
+          if (ok && n > 1) ok = load_tile(s, s.t0 + 1, 0);
+          for (int t = 0; ok && t < n; ++t) {
+            ok = load_tile(s, s.t0 + t, 1);
+            if (ok && t + 2 < n) ok = load_tile(s, s.t0 + t + 2, 0);
+          }
+        }
+      }
+    } else if (warp == 9) {
+      // ---- matrix products
+      const uint32_t q_at = smem_addr(smem);
+      auto advance = [&](int n) {
+        slot += n;
+        if (slot >= L::kSlots) { slot -= L::kSlots; ring_phase ^= 1u; }
+      };
+      // place of the ring `ahead` copies further on
+      auto place = [&](int ahead, int& sl, unsigned& ph) {
+        sl = slot + ahead;
+        ph = ring_phase;
+        if (sl >= L::kSlots) { sl -= L::kSlots; ph ^= 1u; }
+      };
+      auto scores = [&](int st, int sl) {                    // S = Q K^T
+        if (lane == 0) {
+          const uint64_t qd = operand(q_at + (kWide ? st * kTileBytes : 0), 16, 1024);
+          const uint64_t kd = operand(smem_addr(smem + L::kRing + sl * kTileBytes), 16, 1024);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const uint32_t off = (uint32_t)((k >> 2) * (kHalfBytes >> 4) + (k & 3) * 2);
+            mma_ss(tmem + st * kTile, qd + off, kd + off, mma_shape(false), k > 0);
+          }
+        }
+      };
+      auto values = [&](int st, int sl, bool add) {          // O += P V
+        if (lane == 0) {
+          const uint64_t vd = operand(smem_addr(smem + L::kRing + sl * kTileBytes), kHalfBytes, 1024);
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            mma_ts(tmem + 256 + st * kTile, tmem + st * kTile + k * 8, vd + (uint64_t)(k * 128), mma_shape(true), add || k > 0);
+        }
+      };
+      auto commit = [&](uint64_t* bar) {
+        if (lane == 0) tc_commit(bar);
+      };
+      // V rows behind the tile's last token may hold anything, and 0 * NaN must not reach the sums
+      auto clear_tail = [&](const Seg& s, int t, int sl) {
+        const int left = t < s.ctx_tiles ? s.ctx_tokens - t * kTile : s.nd - (t - s.ctx_tiles) * kTile;
+        if (left >= kTile) return;
+        unsigned char* v = smem + L::kRing + sl * kTileBytes;
+        for (int i = lane; i < (kTile - left) * 16; i += 32)
+          *reinterpret_cast<uint4*>(v + ((i >> 3) & 1) * kHalfBytes + (left + (i >> 4)) * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      };
+      for (int i = 0; ok && i < count; ++i) {
+        const Seg s = list[i];
+        if (rb * L::kRows >= s.nd * g) continue;
+        const int n = s.t1 - s.t0;
+        ok = bar_wait(q_full, q_phase, stop);
+        q_phase ^= 1u;
+        if (!ok) break;
+        tc_fence_after();
+        int sl;
+        unsigned ph;
+        if constexpr (kWide) {
+          place(0, sl, ph);
+          if (!(ok = bar_wait(full + sl, ph, stop))) break;
+          scores(0, sl);
+          commit(s_full);
+          scores(1, sl);
+          commit(s_full + 1);
+          commit(empty + sl);
+          advance(1);
+          for (int t = 0; ok && t < n; ++t) {
+            int sv, sk;
+            unsigned pv, pk;
+            place(0, sv, pv);
+            place(1, sk, pk);
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+              if (ok) ok = bar_wait(p_full + st, (p_phase >> st) & 1u, stop);
+              p_phase ^= 1u << st;
+              if (ok && st == 0) {
+                ok = bar_wait(full + sv, pv, stop);
+                if (ok) clear_tail(s, s.t0 + t, sv);
+              }
+              if (!ok) break;
+              tc_fence_after();
+              values(st, sv, t > 0);
+              if (st == 1) commit(empty + sv);
+              if (t + 1 < n) {
+                if (st == 0 && !(ok = bar_wait(full + sk, pk, stop))) break;
+                scores(st, sk);
+                if (st == 1) commit(empty + sk);
+              }
+              commit(s_full + st);
+            }
+            advance(t + 1 < n ? 2 : 1);
+          }
+        } else {
+          for (int st = 0; ok && st < min(n, 2); ++st) {
+            place(0, sl, ph);
+            if (!(ok = bar_wait(full + sl, ph, stop))) break;
+            scores(st, sl);
+            commit(s_full + st);
+            commit(empty + sl);
+            advance(1);
+          }
+          for (int t = 0; ok && t < n; ++t) {
+            const int st = t & 1;
+            ok = bar_wait(p_full + st, (p_phase >> st) & 1u, stop);
+            p_phase ^= 1u << st;
+            place(0, sl, ph);
+            if (ok) ok = bar_wait(full + sl, ph, stop);
+            if (!ok) break;
+            clear_tail(s, s.t0 + t, sl);
+            tc_fence_after();
+            values(st, sl, t > 1);
+            commit(empty + sl);
+            advance(1);
+            if (t + 2 < n) {
+              place(0, sl, ph);
+              if (!(ok = bar_wait(full + sl, ph, stop))) break;
+              scores(st, sl);
+              commit(s_full + st);
+              commit(empty + sl);
+              advance(1);
+            } else {
+              commit(s_full + st);
+            }
+          }
+        }
+      }
+    } else {
+      // ---- softmax
+      const int st = warp >> 2;
+      const uint32_t lane_at = (uint32_t)((warp & 3) * 32) << 16;
+      const uint32_t s_at = tmem + lane_at + st * kTile;
+      const float scale = 0.08838834764831845f * kLog2e;     // 1 / sqrt(128), in the log2 domain
+      for (int i = 0; ok && i < count; ++i) {
+        const Seg s = list[i];
+        const int rows = min(L::kRows, s.nd * g - rb * L::kRows);   // valid rows of this block
+        if (rows <= 0) continue;
+        // the unit's queries, swizzled like the tiles; rows that do not exist are zeros
+        for (int c = tid; c < L::kRows * 16; c += 256) {
+          const int r = c >> 4, ch = c & 15, row = rb * L::kRows + r, t = row / g;
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (r < rows)
+            v = ldg_nc_v4(a.q + (((long long)s.b * a.T + t) * a.geo.Hq + s.kv * g + (row - t * g)) * kHeadDim + ch * 8);
+          *reinterpret_cast<uint4*>(smem + (r >> 7) * kTileBytes + (ch >> 3) * kHalfBytes + (r & 127) * 128 +
+                                    (((ch & 7) ^ (r & 7)) << 4)) = v;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(q_full);
+
+        const int r = (kWide ? st * kTile : 0) + (warp & 3) * 32 + lane;   // this thread's row of the block
+        const int row = rb * L::kRows + r, t_row = row / g, h_row = row - t_row * g;
+        const bool busy = r - lane < rows;                   // some row of the warp exists
+        const int n = s.t1 - s.t0;
+        const int my_n = kWide ? n : (n + 1 - st) >> 1;
+        float m = -INFINITY, l = 0.f;
+        for (int k = 0; k < my_n; ++k) {
+          const int t = s.t0 + (kWide ? k : 2 * k + st);
+          // which of the tile's tokens the row sees
+          uint32_t see[4] = {0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu};
+          bool partial = false;
+          if (busy) {
+            const int at = t < s.ctx_tiles ? t * kTile : (t - s.ctx_tiles) * kTile;
+            const int left = (t < s.ctx_tiles ? s.ctx_tokens : s.nd) - at;
+            if (left < kTile) {
+              partial = true;
+#pragma unroll
+              for (int w = 0; w < 4; ++w) see[w] = left >= 32 * w + 32 ? 0xFFFFFFFFu : left > 32 * w ? (1u << (left - 32 * w)) - 1u : 0u;
+            }
+            if (t >= s.ctx_tiles) {
+              partial = true;
+              if (a.mask == nullptr) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                  const int first = at + 32 * w;
+                  see[w] &= t_row >= first + 31 ? 0xFFFFFFFFu : t_row >= first ? (2u << (t_row - first)) - 1u : 0u;
+                }
+              } else if (t_row < s.nd) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                  see[w] &= at / 32 + w < a.words ? a.mask[((long long)s.b * a.T + t_row) * a.words + at / 32 + w] : 0u;
+              }
+            } else if (a.list != nullptr) {
+              const int2* pages = a.list + (long long)(s.b * Hkv + s.kv) * a.list_cap + t * (kTile / S);
+              const int n_pages = (left + S - 1) / S;
+#pragma unroll
+              for (int w = 0; w < 4; ++w) {
+                if (S == 16) {
+                  const uint32_t lo = 2 * w < n_pages ? (uint32_t)pages[2 * w].y : 0u, hi = 2 * w + 1 < n_pages ? (uint32_t)pages[2 * w + 1].y : 0u;
+                  see[w] &= ((lo >> h_row) & 1u ? 0xFFFFu : 0u) | ((hi >> h_row) & 1u ? 0xFFFF0000u : 0u);
+                } else {
+                  see[w] &= w < n_pages && (((uint32_t)pages[w].y >> h_row) & 1u) ? 0xFFFFFFFFu : 0u;
+                }
+              }
+              partial = true;
+            }
+          }
+          if (!(ok = bar_wait(s_full + st, s_phase, stop))) break;
+          s_phase ^= 1u;
+          tc_fence_after();
+          if (busy) {
+            // a half of the columns at a time (the registers hold one): the second half is looked over for its maximum,
+            // the first looked over and kept, the second read again when its turn comes
+            uint32_t x[2][32];
+            auto fetch = [&](int half) {
+              tmem_ld32(x[0], s_at + 64 * half);
+              tmem_ld32(x[1], s_at + 64 * half + 32);
+              tmem_wait_ld();
+              if (partial) {
+#pragma unroll
+                for (int w = 0; w < 2; ++w)
+#pragma unroll
+                  for (int e = 0; e < 32; ++e)
+                    if (!((see[2 * half + w] >> e) & 1u)) x[w][e] = 0xFF800000u;   // -inf, whatever the padding held
+              }
+            };
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int half = 1; half >= 0; --half) {
+              fetch(half);
+#pragma unroll
+              for (int w = 0; w < 2; ++w)
+#pragma unroll
+                for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(x[w][e]));
+            }
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+            if (k == 0) {
+              m = top;
+            } else {
+              const bool raise = top > m + kMaxSlack;        // (m = -inf: any finite value)
+              if (__any_sync(0xFFFFFFFFu, raise)) {
+                const float factor = raise ? exp2_fast(m - top) : 1.f;
+                if (raise) m = top;
+                l *= factor;
+                const uint32_t o_at = tmem + lane_at + 256 + st * kTile;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                  uint32_t o[32];
+                  tmem_ld32(o, o_at + 32 * w);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                  tmem_st32(o_at + 32 * w, o);
+                }
+                tmem_wait_st();
+              }
+            }
+            const float ref = m == -INFINITY ? 0.f : -m;
+            // P is rounded to bf16 for the matrix product with V (half a step, 2^-9 of each weight); the sum keeps fp32
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              if (half == 1) fetch(1);
+              uint32_t p[32];
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                const float p0 = exp2_fast(fmaf(__uint_as_float(x[e >> 4][(2 * e) & 31]), scale, ref));
+                const float p1 = exp2_fast(fmaf(__uint_as_float(x[e >> 4][(2 * e + 1) & 31]), scale, ref));
+                sum[e & 1] += p0;
+                sum[2 + (e & 1)] += p1;
+                const __nv_bfloat162 pair = __floats2bfloat162_rn(p0, p1);
+                p[e] = *reinterpret_cast<const uint32_t*>(&pair);
+              }
+              tmem_st32(s_at + 32 * half, p);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_wait_st();
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(p_full + st);
+        }
+        if (!ok) break;
+        if (my_n > 0) {
+          if (!(ok = bar_wait(s_full + st, s_phase, stop))) break;   // the last product with V is complete
+          s_phase ^= 1u;
+        }
+        // up to 128 rows: both streams hold sums of the same rows; each warp joins 64 of the coordinates
+        float a_own = 1.f, a_other = 0.f;
+        if constexpr (!kWide) {
+          ml[st * kTile + (warp & 3) * 32 + lane] = make_float2(m, l);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(joined);
+          if (!(ok = bar_wait(joined, j_phase, stop))) break;
+          j_phase ^= 1u;
+          const float2 o = ml[(st ^ 1) * kTile + (warp & 3) * 32 + lane];
+          const float both = fmaxf(m, o.x);
+          a_own = m == -INFINITY ? 0.f : exp2_fast(m - both);
+          a_other = o.x == -INFINITY ? 0.f : exp2_fast(o.x - both);
+          l = l * a_own + o.y * a_other;
+          m = both;
+        }
+        tc_fence_after();
+        if (busy) {
+          const bool whole = s.t0 == 0 && s.last;
+          const float inv = l > 0.f ? 1.f / l : 0.f;
+          const long long part = (long long)(blockIdx.x * 2 + (i == 0 && first_list ? 0 : 1)) * L::kRows + r;
+          const long long at = ((long long)s.b * a.T + t_row) * a.geo.Hq + s.kv * g + h_row;
+          const bool other_on = !kWide && n > 1;             // (a stream without a tile has written no O)
+          const bool own_on = kWide || my_n > 0;
+#pragma unroll
+          for (int w = 0; w < (kWide ? 4 : 2); ++w) {
+            const int col = kWide ? 32 * w : 64 * st + 32 * w;
+            uint32_t o[32], o2[32];
+            tmem_ld32(o, tmem + lane_at + 256 + st * kTile + col);
+            if constexpr (!kWide) tmem_ld32(o2, tmem + lane_at + 256 + (st ^ 1) * kTile + col);
+            tmem_wait_ld();
+            float f[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              if constexpr (kWide) {
+                f[e] = __uint_as_float(o[e]);
+              } else {
+                f[e] = (own_on ? __uint_as_float(o[e]) * a_own : 0.f) +
+                       ((st == 0 ? other_on : true) ? __uint_as_float(o2[e]) * a_other : 0.f);
+              }
+            }
+            if (r < rows) {
+              if (whole) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                  uint4 v;
+                  uint32_t* pv = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+                  for (int z = 0; z < 4; ++z) {
+                    const __nv_bfloat162 pair = __floats2bfloat162_rn(f[e + 2 * z] * inv, f[e + 2 * z + 1] * inv);
+                    pv[z] = *reinterpret_cast<const uint32_t*>(&pair);
+                  }
+                  *reinterpret_cast<uint4*>(a.out + at * kHeadDim + col + e) = v;
+                }
+              } else {
+#pragma unroll
+                for (int e = 0; e < 32; e += 4)
+                  __stcg(reinterpret_cast<float4*>(a.part_o + part * kHeadDim + col + e), make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]));
+              }
+            }
+          }
+          if (r < rows && (kWide || st == 0)) {
+            if (whole) a.lse[at] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+            else __stcg(a.part_ml + part, make_float2(m, l));
+          }
+        }
+        if constexpr (!kWide) {
+          // the other stream's warps read this stream's (m, l) and O: they have, once all have joined again
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(joined);
+          if (!(ok = bar_wait(joined, j_phase, stop))) break;
+          j_phase ^= 1u;
+        } else {
+          // Q may be overwritten once both streams have seen their last scores
+          __syncwarp();
+          if (lane == 0) bar_arrive(joined);
+          if (!(ok = bar_wait(joined, j_phase, stop))) break;
+          j_phase ^= 1u;
+        }
+      }
+    }
+    first_list = false;
+    __syncthreads();
+    if (*stop != 0) break;
+  }
+
+  if (*stop != 0) {
+    // a wait ran out: copies and products under way still write to this CTA's memory
+    if (tid == 0) atomicOr(a.status, SWARM_DEV_TIMEOUT);
+    if (warp == 8) {
+      for (int i = 0; i < min(issued, L::kSlots); ++i) {
+        if (--slot < 0) { slot = L::kSlots - 1; ring_phase ^= 1u; }
+        for (unsigned polls = 0; polls < kWaitLimit && !bar_try(full + slot, ring_phase); ++polls) { }
+      }
+    }
+    if (warp == 9) {
+      if (lane == 0) tc_commit(drained);
+      for (unsigned polls = 0; polls < kWaitLimit && !bar_try(drained, 0u); ++polls) { }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  }
+}
+
+// Joins the partial sums of the units that were cut: a warp per row, four coordinates per lane.
+template <int kRows>
+__global__ void __launch_bounds__(256)
+tree_merge_kernel(const TreeArgs a) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const long long at = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);   // [B][T][Hq]
+  if (at >= (long long)a.geo.B * a.T * a.geo.Hq) return;
+  const int h = (int)(at % a.geo.Hq), t = (int)(at / a.geo.Hq % a.T), b = (int)(at / a.geo.Hq / a.T);
+  const int kv = h / a.geo.g, u = b * a.geo.Hkv + kv;
+  int ctx, nd;
+  bool bad;
+  unit_lengths(a, u, ctx, nd, bad);
+  if (t >= nd) return;
+  const int first = a.unit_first[u], c0 = first >> 1, n = a.unit_last[u] - c0 + 1;
+  if (n == 1) return;                                        // written by the CTA that had the whole unit
+  const int row = t * a.geo.g + (h - kv * a.geo.g), rb = row / kRows, r = row - rb * kRows;
+  auto part = [&](int i) {
+    return ((long long)((c0 + i) * a.row_blocks + rb) * 2 + (i == 0 ? first & 1 : 0)) * kRows + r;
+  };
+  float M = -INFINITY;
+  for (int i = lane; i < n; i += 32) M = fmaxf(M, __ldcg(a.part_ml + part(i)).x);
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
+  const float ref = M == -INFINITY ? 0.f : M;
+  float sum = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    const float2 ml = i0 + lane < n ? __ldcg(a.part_ml + part(i0 + lane)) : make_float2(-INFINITY, 0.f);
+    const float w = exp2_fast(ml.x - ref);
+    sum += ml.y * w;
+    const int here = min(32, n - i0);
+    for (int i = 0; i < here; i += 8) {
+      float4 v[8];
+#pragma unroll
+      for (int z = 0; z < 8; ++z)
+        v[z] = i + z < here ? __ldcg(reinterpret_cast<const float4*>(a.part_o + part(i0 + i + z) * kHeadDim) + lane)
+                            : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int z = 0; z < 8; ++z) {
+        const float wz = __shfl_sync(0xFFFFFFFFu, w, (i + z) & 31);
+        if (i + z < here) {
+          o.x = fmaf(v[z].x, wz, o.x); o.y = fmaf(v[z].y, wz, o.y); o.z = fmaf(v[z].z, wz, o.z); o.w = fmaf(v[z].w, wz, o.w);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int s = 16; s >= 1; s >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x * inv, o.y * inv), hi = __floats2bfloat162_rn(o.z * inv, o.w * inv);
+  reinterpret_cast<uint2*>(a.out + at * kHeadDim)[lane] =
+      make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+  if (lane == 0) a.lse[at] = sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
+}
+
+// The pages that the heads of a KV head have selected, ascending, each with the heads that did: a CTA per unit.  The
+// union is a bitmap in shared memory; a page's place in the list is the number of set bits below it.
+__global__ void __launch_bounds__(256)
+tree_list_kernel(const TreeArgs a, const int32_t* __restrict__ sel, const int32_t* __restrict__ n_sel, int2* __restrict__ list,
+                 int32_t* __restrict__ list_tokens) {
+  extern __shared__ uint32_t s_map[];                        // [words] bits, then [words] set bits in front
+  __shared__ int s_sum[8];
+  const int u = blockIdx.x, b = u / a.geo.Hkv, kv = u - b * a.geo.Hkv, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int words = (a.geo.Pmax + 31) / 32;
+  int* s_before = reinterpret_cast<int*>(s_map + words);
+  for (int i = tid; i < words; i += 256) s_map[i] = 0u;
+  pdl_wait();
+  pdl_launch_dependents();
+  __syncthreads();
+  const int S = a.geo.S, len = a.ctx_len[b];
+  const long long owned = a.page_base[b + 1] - a.page_base[b];
+  const int P = len < 0 || pages_of(len, S) > owned ? 0 : min(pages_of(len, S), a.geo.Pmax);
+  const int k = a.geo.k;
+  auto each = [&](auto&& f) {                                // every selected page of the group's heads
+    for (int j = tid; j < a.geo.g * k; j += 256) {
+      const int hh = j / k, at = j - hh * k;
+      const long long bh = (long long)b * a.geo.Hq + kv * a.geo.g + hh;
+      if (at < n_sel[bh]) f(hh, sel[bh * k + at]);
+    }
+  };
+  each([&](int, int p) {
+    if (p < 0 || p >= P) atomicOr(a.status, SWARM_DEV_BAD_PAGE);
+    else atomicOr(s_map + (p >> 5), 1u << (p & 31));
+  });
+  __syncthreads();
+  const int per = (words + 255) / 256, lo = min(words, tid * per), hi = min(words, lo + per);
+  int mine = 0;
+  for (int w = lo; w < hi; ++w) mine += __popc(s_map[w]);
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 31) s_sum[warp] = incl;
+  __syncthreads();
+  int at = incl - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    if (w < warp) at += s_sum[w];
+    total += s_sum[w];
+  }
+  int2* row = list + (long long)u * a.list_cap;
+  for (int w = lo; w < hi; ++w) {
+    s_before[w] = at;
+    for (uint32_t bits = s_map[w]; bits != 0u; bits &= bits - 1u) row[at++] = make_int2(32 * w + __ffs(bits) - 1, 0);
+  }
+  __syncthreads();
+  each([&](int hh, int p) {
+    if (p >= 0 && p < P)
+      atomicOr(reinterpret_cast<unsigned*>(&row[s_before[p >> 5] + __popc(s_map[p >> 5] & ((1u << (p & 31)) - 1u))].y), 1u << hh);
+  });
+  if (tid == 0) {
+    const bool ends = P > 0 && ((s_map[(P - 1) >> 5] >> ((P - 1) & 31)) & 1u);
+    list_tokens[u] = total * S - (ends ? P * S - len : 0);
+  }
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------------------
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn g_encode = nullptr;
+
+// bf16 tensor of five dimensions, the first of 64 coordinates, boxes with the 128-byte swizzle.  Strides in bytes.
+cudaError_t make_map(CUtensorMap* map, const void* base, const cuuint64_t (&dims)[5], const cuuint64_t (&strides)[4], const cuuint32_t (&box)[5]) {
+  if (g_encode == nullptr) return cudaErrorNotSupported;
+  const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  const CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+constexpr int64_t align256(int64_t x) { return (x + 255) & ~int64_t(255); }
+
+struct TreeLayout {
+  int64_t part_o, part_ml, unit_first, unit_last, list, list_tokens, total;
+  int list_cap;
+};
+TreeLayout tree_layout(const Geometry& geo, int T) {
+  TreeLayout l;
+  const int64_t units = (int64_t)geo.B * geo.Hkv, rows_all = (int64_t)T * geo.g;
+  const int64_t rows = rows_all > kTile ? 2 * kTile : kTile;
+  const int64_t ctas = std::max<int64_t>(kMaxTreeCtas, (rows_all + rows - 1) / rows);
+  l.list_cap = (int)std::min<int64_t>((int64_t)geo.g * geo.k, geo.Pmax);
+  l.part_o = 0;
+  l.part_ml = align256(l.part_o + ctas * 2 * rows * kHeadDim * 4);
+  l.unit_first = align256(l.part_ml + ctas * 2 * rows * 8);
+  l.unit_last = align256(l.unit_first + units * 4);
+  l.list_tokens = align256(l.unit_last + units * 4);
+  l.list = align256(l.list_tokens + units * 4);
+  l.total = align256(l.list + units * l.list_cap * 8);
+  return l;
+}
+
+}  // namespace
+
+bool tree_supported(const Geometry& geo, int T, bool selected) {
+  if ((int64_t)T * geo.g >= (int64_t(1) << 30) || geo.n_pool_pages >= (int64_t(1) << 31) || (int64_t)geo.B * T * geo.Hq >= (int64_t(1) << 33))
+    return false;
+  return !selected || (geo.g <= 32 && (geo.Pmax + 31) / 32 * 8 <= kMaxTreeMapBytes);
+}
+
+long long tree_attn_workspace_bytes(const Geometry& geo, int T) { return tree_layout(geo, T).total; }
+
+cudaError_t configure_tree() {
+  void* p = nullptr;
+  cudaDriverEntryPointQueryResult q;
+  cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q);
+  if (e != cudaSuccess || q != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
+  g_encode = reinterpret_cast<EncodeTiledFn>(p);
+  e = cudaFuncSetAttribute(tree_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<false>::kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(tree_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<true>::kBytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(tree_list_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxTreeMapBytes);
+  return e;
+}
+
+cudaError_t launch_tree_attn(const Geometry& geo, const TreeCall& c, void* workspace, uint32_t* status, cudaStream_t st) {
+  const TreeLayout lay = tree_layout(geo, c.T);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  TreeArgs a{};
+  a.geo = geo;
+  a.q = c.q;
+  a.page_base = c.page_base;
+  a.ctx_len = c.ctx_len;
+  a.n_draft = c.n_draft;
+  a.mask = c.mask;
+  a.T = c.T;
+  a.words = (c.T + 31) / 32;
+  a.part_o = reinterpret_cast<float*>(ws + lay.part_o);
+  a.part_ml = reinterpret_cast<float2*>(ws + lay.part_ml);
+  a.unit_first = reinterpret_cast<int32_t*>(ws + lay.unit_first);
+  a.unit_last = reinterpret_cast<int32_t*>(ws + lay.unit_last);
+  a.list_cap = lay.list_cap;
+  a.out = c.out;
+  a.lse = c.lse;
+  a.status = status;
+
+  const cuuint64_t row = kHeadDim * 2, S = (cuuint64_t)geo.S, Hkv = (cuuint64_t)geo.Hkv, T = (cuuint64_t)c.T;
+  // pool: (64 coordinates, token of the page, page, half of the coordinates, KV head and K or V)
+  CUtensorMap tile, page, dk, dv;
+  const cuuint64_t pool_dims[5] = {64, S, (cuuint64_t)geo.n_pool_pages, 2, Hkv * 2};
+  const cuuint64_t pool_strides[4] = {row, Hkv * 2 * S * row, 128, S * row};
+  const cuuint32_t tile_box[5] = {64, (cuuint32_t)S, (cuuint32_t)(kTile / S), 2, 1}, page_box[5] = {64, (cuuint32_t)S, 1, 1, 1};
+  cudaError_t e = make_map(&tile, c.kv_pool, pool_dims, pool_strides, tile_box);
+  if (e == cudaSuccess) e = make_map(&page, c.kv_pool, pool_dims, pool_strides, page_box);
+  // drafted tokens: (64 coordinates, token, half of the coordinates, KV head, request)
+  const cuuint64_t draft_dims[5] = {64, T, 2, Hkv, (cuuint64_t)geo.B};
+  const cuuint64_t draft_strides[4] = {Hkv * row, 128, row, T * Hkv * row};
+  const cuuint32_t draft_box[5] = {64, (cuuint32_t)kTile, 2, 1, 1};
+  if (e == cudaSuccess) e = make_map(&dk, c.k, draft_dims, draft_strides, draft_box);
+  if (e == cudaSuccess) e = make_map(&dv, c.v, draft_dims, draft_strides, draft_box);
+  if (e != cudaSuccess) return e;
+
+  if (c.sel != nullptr) {
+    int2* list = reinterpret_cast<int2*>(ws + lay.list);
+    int32_t* tokens = reinterpret_cast<int32_t*>(ws + lay.list_tokens);
+    e = launch_pdl(tree_list_kernel, dim3((unsigned)(geo.B * geo.Hkv)), dim3(256), (size_t)((geo.Pmax + 31) / 32) * 8, st, true, a, c.sel,
+                   c.n_sel, list, tokens);
+    if (e != cudaSuccess) return e;
+    a.list = list;
+    a.list_tokens = tokens;
+  }
+  const int64_t rows = (int64_t)c.T * geo.g;
+  const bool wide = rows > kTile;
+  a.row_blocks = wide ? (int)((rows + 2 * kTile - 1) / (2 * kTile)) : 1;
+  const int64_t most = (int64_t)geo.B * geo.Hkv * (((int64_t)geo.Pmax * geo.S + kTile - 1) / kTile + (c.T + kTile - 1) / kTile);
+  a.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kMaxTreeCtas, sm_count()) / a.row_blocks, most));
+  const unsigned grid = (unsigned)(a.chunks * a.row_blocks);
+  e = wide ? launch_pdl(tree_attn_kernel<true>, dim3(grid), dim3(kThreads), (size_t)Layout<true>::kBytes, st, true, tile, page, dk, dv, a)
+           : launch_pdl(tree_attn_kernel<false>, dim3(grid), dim3(kThreads), (size_t)Layout<false>::kBytes, st, true, tile, page, dk, dv, a);
+  if (e != cudaSuccess) return e;
+  const int64_t out_rows = (int64_t)geo.B * c.T * geo.Hq;
+  const dim3 merge_grid((unsigned)((out_rows + 7) / 8));
+  return wide ? launch_pdl(tree_merge_kernel<2 * kTile>, merge_grid, dim3(256), 0, st, true, a)
+              : launch_pdl(tree_merge_kernel<kTile>, merge_grid, dim3(256), 0, st, true, a);
+}
+
+}  // namespace swarm
