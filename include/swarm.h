@@ -48,6 +48,12 @@ extern "C" {
 #define SWARM_DEV_BAD_REPLICA 4u        /* replica mask is 0 or names a queue >= n_queues          */
 #define SWARM_DEV_BAD_LENGTH 8u         /* ctx_len < 1 or more pages than the request owns         */
 #define SWARM_DEV_TIMEOUT 16u           /* a bounded wait expired (a copy, or a hand-off between kernels) */
+#define SWARM_DEV_BAD_TOKEN 32u         /* an accepted path names a token that is not there        */
+
+/* ---- types of the logits of swarm_beam_select -------------------------------------------- */
+#define SWARM_DTYPE_F32 0
+#define SWARM_DTYPE_BF16 1
+#define SWARM_DTYPE_F16 2
 
 /* ---- flags in swarm_shape.flags --------------------------------------------------------- */
 #define SWARM_ORDER_BY_ID 1u            /* schedule clusters by id only (default: by number of
@@ -148,6 +154,48 @@ typedef struct swarm_tree {
   int32_t max_draft;       /* T                                                                              */
   int32_t reserved;        /* must be 0                                                                      */
 } swarm_tree;
+
+/* New tokens of a batch of requests, see swarm_append_tokens.  Device pointers. */
+typedef struct swarm_new_tokens {
+  const void* k;           /* bf16 [B][T][Hkv][d]                                                            */
+  const void* v;           /* bf16 [B][T][Hkv][d]                                                            */
+  const int32_t* n_new;    /* [B] tokens each request takes over: 0..max_path, without a path 0..T           */
+  const int32_t* path;     /* [B][max_path] which of the T they are, in their new order (the accepted path   */
+                           /* of a drafted tree); entries from n_new[b] on are not read.  NULL: the first ones */
+  int32_t max_new;         /* T                                                                              */
+  int32_t max_path;        /* 0 without a path                                                               */
+} swarm_new_tokens;
+
+/* A new layout of the cache, see swarm_plan_pages.  Device pointers. */
+typedef struct swarm_page_plan {
+  const int64_t* page_base;   /* [B+1] the present layout                                                    */
+  const int32_t* ctx_len;     /* [B]   (0 is allowed)                                                        */
+  const int32_t* parent;      /* [B] new request j continues old request parent[j]; -1: j starts empty       */
+  const int32_t* reserve;     /* [B] spare pages behind the pages of new request j; NULL: none               */
+  const uint8_t* keep;        /* [n_pool_pages] 0 = the page is dropped; NULL: every page is kept            */
+  int64_t* new_page_base;     /* [B+1]                                                                       */
+  int32_t* new_ctx_len;       /* [B]                                                                         */
+  int32_t* src;               /* [max_moves] the page moves: pool page src[i] goes to dst[i], dst ascending  */
+  int32_t* dst;               /* [max_moves]                                                                 */
+  int32_t* n_moves;           /* [1] their number (pages that stay where they are included), -1: refused     */
+  int32_t max_moves;          /* capacity of src and dst                                                     */
+  int32_t in_place;           /* 1: for moves inside one pool                                                */
+} swarm_page_plan;
+
+/* Page moves, see swarm_move_pages.  Device pointers. */
+typedef struct swarm_page_moves {
+  const int32_t* src;         /* [max_moves]                                                                 */
+  const int32_t* dst;         /* [max_moves]                                                                 */
+  const int32_t* n_moves;     /* [1]                                                                         */
+  const void* from_pool;      /* bf16 [n_pool_pages][Hkv][2][S][d]                                           */
+  void* to_pool;              /* the same pool, or another one of the same shape                             */
+  const void* from_ksum;      /* bf16 [n_pool_pages][Hkv][2][d]; both NULL: summaries are not moved          */
+  void* to_ksum;
+  const int32_t* from_page2cluster;   /* [n_pool_pages]; both NULL: not moved                                */
+  int32_t* to_page2cluster;
+  int32_t max_moves;
+  int32_t reserved;           /* must be 0                                                                   */
+} swarm_page_moves;
 
 /* Lifetime.  swarm_create validates the shape and allocates only host memory.
  * The CUDA device current at creation must stay current for every later call with this ctx. */
@@ -431,6 +479,58 @@ int32_t swarm_build_clusters(const float* dist, int32_t n_entries, float tau, vo
 int64_t swarm_tree_attn_workspace_bytes(const swarm_shape* shape, int32_t max_draft);
 int32_t swarm_tree_attn(swarm_ctx* ctx, const swarm_inputs* inputs, const swarm_tree* tree, const int32_t* sel,
                         const int32_t* n_sel, void* workspace, int64_t workspace_bytes, void* out, float* lse, void* stream);
+
+/* Writes new tokens behind the ones each request has: token i < n_new[b] of request b goes to position ctx_len[b] + i, its
+ * key and value rows into the page page_base[b] + position / S, and ctx_len_out[b] = ctx_len[b] + n_new[b] (ctx_len_out
+ * may be inputs->ctx_len itself).  With ksum the summaries of the pages written to are brought up to date: they must
+ * describe the tokens that those pages held, as swarm_build_summaries or earlier calls left them.  For decoded tokens, for
+ * the accepted path of a drafted tree (new->path; a token may be named twice) and for prompts.
+ * A request whose new length does not fit the pages it owns (or with n_new out of range) sets SWARM_DEV_BAD_LENGTH and
+ * is left as it was.  A path entry outside 0..T-1 sets SWARM_DEV_BAD_TOKEN; its rows are written as zeros.
+ * Reads inputs->page_base, ctx_len.  kv_pool as in swarm_inputs, ksum bf16 [n_pool_pages][Hkv][2][d] or NULL. */
+int32_t swarm_append_tokens(swarm_ctx* ctx, const swarm_inputs* inputs, const swarm_new_tokens* tokens, void* kv_pool,
+                            void* ksum, int32_t* ctx_len_out, void* stream);
+
+/* Plans a new layout of the cache: the page ranges stay contiguous, so freeing, forking, reordering, thinning out and growing
+ * requests all mean new ranges and page moves.  New request j holds the kept pages of old request parent[j] in their
+ * order (several j may name the same parent: a fork; a request that no j names is freed) and reserve[j] spare pages:
+ *   new_page_base[j+1] = new_page_base[j] + kept pages + reserve[j], from new_page_base[0] = 0,
+ *   new_ctx_len[j] = tokens of the kept pages (a partial last page that is kept stays the last).
+ * Dropping pages shortens the sequence; keys are moved as they are.
+ * Refused as a whole (n_moves = -1, the new tables repeat the present layout, nothing is to be moved) and reported:
+ * parent outside -1..B-1 or, in_place, not strictly ascending over the requests that have one (SWARM_DEV_BAD_PAGE: forks
+ * and reorders need a second pool); a length that does not fit its pages, reserve < 0, a new layout beyond
+ * n_pool_pages, more than max_moves moves (SWARM_DEV_BAD_LENGTH).
+ * The outputs must not overlap the inputs.  SWARM_ERR_UNSUPPORTED: n_pool_pages >= 2^30. */
+int32_t swarm_plan_pages(swarm_ctx* ctx, const swarm_page_plan* plan, void* stream);
+
+/* Moves pages: K/V, summaries and page2cluster entries of pool page src[i] to dst[i] for i < min(n_moves, max_moves); a negative
+ * n_moves moves nothing.  Pages that no dst names are left as they were.
+ * Between two pools (to_pool != from_pool; all tables must then be different ones) the pairs are independent.  Inside one
+ * pool (all tables the same) the result is that of reading every source before writing any destination, provided that,
+ * with the pairs of dst < src taken first to last and then those of dst > src last to first, no pair writes a page that a later
+ * one reads: true for every plan of swarm_plan_pages, and for copies to pages that are not sources.  A pair that breaks this,
+ * a second pair with the same dst, and ids outside the pool set SWARM_DEV_BAD_PAGE and are skipped.
+ * workspace: swarm_move_pages_workspace_bytes(shape) bytes of device memory (256-byte aligned, contents irrelevant), used by
+ * one call at a time; < 0: minus an error code. */
+int64_t swarm_move_pages_workspace_bytes(const swarm_shape* shape);
+int32_t swarm_move_pages(swarm_ctx* ctx, const swarm_page_moves* moves, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Beam search's selection (no ctx).  Of all continuations of a prompt by a token of one of its beams the n_keep with the largest
+ *   score[b][k] + logits[b][k][v] - log sum_v' exp(logits[b][k][v'])
+ * in descending order, ties to the lowest k * vocab + v (compared in 64 bits):
+ *   new_score[b][i] that sum, parent[b][i] = b * n_beams + k (the row of the beam it continues, as swarm_plan_pages takes it),
+ *   token[b][i] = v.
+ * Continuations of -inf or NaN are never chosen; where fewer than n_keep are left, new_score = -inf, parent = token = -1.
+ * Logits must be below +inf.  logits: SWARM_DTYPE_*, row (b, k) starts (b * n_beams + k) * row_stride elements behind the
+ * first (row_stride >= vocab).  score f32 [batch][n_beams]; outputs [batch][n_keep]; 1 <= n_keep <= 64.
+ * workspace: swarm_beam_select_workspace_bytes bytes of device memory (contents irrelevant), used by one call at a time;
+ * < 0: minus an error code.  SWARM_ERR_UNSUPPORTED: n_beams * vocab >= 2^31, or too many candidates
+ * (n_beams * vocab / 8192 * n_keep^2 beyond about 6 million). */
+int64_t swarm_beam_select_workspace_bytes(int32_t batch, int32_t n_beams, int32_t vocab, int32_t n_keep);
+int32_t swarm_beam_select(const void* logits, int32_t dtype, int64_t row_stride, const float* score, int32_t batch,
+                          int32_t n_beams, int32_t vocab, int32_t n_keep, void* workspace, int64_t workspace_bytes,
+                          float* new_score, int32_t* parent, int32_t* token, void* stream);
 
 /* End-to-end convenience for callers holding the per-step data in HOST memory (pinned memory
  * recommended): copies q_host (bf16 [B][Hq][d]) into the ctx's staging area, runs swarm_step with

@@ -19,6 +19,7 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE_TOO_SMALL, ERR_CUDA = 0, 1, 
 ERR_STATIC_SCRATCH_TOO_SMALL = 5
 STATIC_MAX_HEADS = 2048
 DEV_BAD_PAGE, DEV_BAD_CLUSTER, DEV_BAD_REPLICA, DEV_BAD_LENGTH, DEV_TIMEOUT = 1, 2, 4, 8, 16
+DEV_BAD_TOKEN = 32
 ORDER_BY_ID, UNIT_LOAD = 1, 2
 SCORER_AUTO, SCORER_TENSOR, SCORER_FP32 = 0, 1, 2
 _ERR_NAMES = {1: "INVALID_ARG", 2: "UNSUPPORTED", 3: "WORKSPACE_TOO_SMALL", 4: "CUDA",
@@ -32,7 +33,9 @@ EXPORTS = (
     "swarm_build_clusters_workspace_bytes", "swarm_build_clusters",
     "swarm_cache_admit_workspace_bytes", "swarm_cache_admit",
     "swarm_step_begin", "swarm_step_end", "swarm_cluster_flags",
-    "swarm_tree_attn_workspace_bytes", "swarm_tree_attn",
+    "swarm_tree_attn_workspace_bytes", "swarm_tree_attn", "swarm_append_tokens",
+    "swarm_plan_pages", "swarm_move_pages_workspace_bytes", "swarm_move_pages",
+    "swarm_beam_select_workspace_bytes", "swarm_beam_select",
 )
 
 
@@ -83,6 +86,8 @@ def load_library() -> ctypes.CDLL:
         lib.swarm_build_clusters_workspace_bytes.restype = ctypes.c_int64
         lib.swarm_cache_admit_workspace_bytes.restype = ctypes.c_int64
         lib.swarm_tree_attn_workspace_bytes.restype = ctypes.c_int64
+        lib.swarm_move_pages_workspace_bytes.restype = ctypes.c_int64
+        lib.swarm_beam_select_workspace_bytes.restype = ctypes.c_int64
         v, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
         lib.swarm_build_clusters.argtypes = [v, i32, ctypes.c_float, v, i64, v, v, v, i64, v, v, v, v]
         _lib = lib
@@ -466,6 +471,145 @@ def swarm_tree_attn(ctx, inputs: swarm_inputs, tree: swarm_tree, sel: Optional[t
                                         _ptr(lse, "lse"), _stream(stream))
     if rc != OK:
         _check(rc, "swarm_tree_attn", ctx)
+
+
+class swarm_new_tokens(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "n_new", "path")] + \
+               [("max_new", ctypes.c_int32), ("max_path", ctypes.c_int32)]
+
+
+class swarm_page_plan(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("page_base", "ctx_len", "parent", "reserve", "keep", "new_page_base",
+                                               "new_ctx_len", "src", "dst", "n_moves")] + \
+               [("max_moves", ctypes.c_int32), ("in_place", ctypes.c_int32)]
+
+
+class swarm_page_moves(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("src", "dst", "n_moves", "from_pool", "to_pool", "from_ksum", "to_ksum",
+                                               "from_page2cluster", "to_page2cluster")] + \
+               [("max_moves", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+def make_new_tokens(*, k: torch.Tensor, v: torch.Tensor, n_new: torch.Tensor,
+                    path: Optional[torch.Tensor] = None) -> swarm_new_tokens:
+    """Tokens to append: k and v bf16 [B, T, Hkv, 128], n_new int32 [B], path int32 [B, max_path] (which of the T tokens, in
+    their new order) or None for the first n_new.  The caller keeps the tensors alive while the struct is in use."""
+    if k.dim() != 4:
+        raise ValueError("k must have four dimensions: request, token, head, coordinate")
+    batch, T = k.shape[:2]
+    _expect(k, "k", torch.bfloat16, (batch, T, k.shape[2], 128))
+    _expect(v, "v", torch.bfloat16, k.shape)
+    _expect(n_new, "n_new", torch.int32, (batch,))
+    if path is not None:
+        _expect(path, "path", torch.int32, (batch, path.shape[-1]))
+    return swarm_new_tokens(_ptr(k, "k"), _ptr(v, "v"), _ptr(n_new, "n_new"), _ptr(path, "path"), T,
+                            0 if path is None else path.shape[1])
+
+
+def swarm_append_tokens(ctx, inputs: swarm_inputs, tokens: swarm_new_tokens, kv_pool: torch.Tensor,
+                        ksum: Optional[torch.Tensor], ctx_len_out: torch.Tensor, stream=None) -> None:
+    """Writes the new tokens behind each request's, updates the summaries of the pages reached (ksum may be None) and writes
+    the new lengths (ctx_len_out may be the tensor that inputs.ctx_len points to)."""
+    rc = load_library().swarm_append_tokens(ctx, ctypes.byref(inputs), ctypes.byref(tokens), _ptr(kv_pool, "kv_pool"),
+                                            _ptr(ksum, "ksum"), _ptr(ctx_len_out, "ctx_len_out"), _stream(stream))
+    if rc != OK:
+        _check(rc, "swarm_append_tokens", ctx)
+
+
+def make_page_plan(*, page_base: torch.Tensor, ctx_len: torch.Tensor, parent: torch.Tensor, new_page_base: torch.Tensor,
+                   new_ctx_len: torch.Tensor, src: torch.Tensor, dst: torch.Tensor, n_moves: torch.Tensor,
+                   reserve: Optional[torch.Tensor] = None, keep: Optional[torch.Tensor] = None,
+                   in_place: bool = False) -> swarm_page_plan:
+    """A new layout of the cache (see swarm_plan_pages): int64 page_base / new_page_base [B+1], int32 for the others, uint8
+    keep [n_pool_pages].  src and dst have room for the page moves.  The caller keeps the tensors alive."""
+    batch = parent.numel()
+    for name, t, dtype, n in (("page_base", page_base, torch.int64, batch + 1), ("ctx_len", ctx_len, torch.int32, batch),
+                              ("parent", parent, torch.int32, batch), ("new_page_base", new_page_base, torch.int64, batch + 1),
+                              ("new_ctx_len", new_ctx_len, torch.int32, batch), ("dst", dst, torch.int32, src.numel()),
+                              ("src", src, torch.int32, src.numel())):
+        _expect(t, name, dtype, (n,))
+    if reserve is not None:
+        _expect(reserve, "reserve", torch.int32, (batch,))
+    if keep is not None:
+        _expect(keep, "keep", torch.uint8, (keep.numel(),))
+    return swarm_page_plan(*[_ptr(t, n) for n, t in (("page_base", page_base), ("ctx_len", ctx_len), ("parent", parent),
+                                                     ("reserve", reserve), ("keep", keep), ("new_page_base", new_page_base),
+                                                     ("new_ctx_len", new_ctx_len), ("src", src), ("dst", dst),
+                                                     ("n_moves", n_moves))], src.numel(), 1 if in_place else 0)
+
+
+def swarm_plan_pages(ctx, plan: swarm_page_plan, stream=None) -> None:
+    rc = load_library().swarm_plan_pages(ctx, ctypes.byref(plan), _stream(stream))
+    if rc != OK:
+        _check(rc, "swarm_plan_pages", ctx)
+
+
+def make_page_moves(*, src: torch.Tensor, dst: torch.Tensor, n_moves: torch.Tensor, from_pool: torch.Tensor, to_pool: torch.Tensor,
+                    from_ksum: Optional[torch.Tensor] = None, to_ksum: Optional[torch.Tensor] = None,
+                    from_page2cluster: Optional[torch.Tensor] = None,
+                    to_page2cluster: Optional[torch.Tensor] = None) -> swarm_page_moves:
+    """Page moves (see swarm_move_pages): int32 src and dst, inside one pool or between two.  The caller keeps the tensors
+    alive while the struct is in use."""
+    _expect(src, "src", torch.int32, (src.numel(),))
+    _expect(dst, "dst", torch.int32, (src.numel(),))
+    for name, a, b in (("pool", from_pool, to_pool), ("ksum", from_ksum, to_ksum), ("page2cluster", from_page2cluster, to_page2cluster)):
+        if a is not None and b is not None:
+            _expect(b, f"to_{name}", a.dtype, a.shape)
+    return swarm_page_moves(*[_ptr(t, n) for n, t in (("src", src), ("dst", dst), ("n_moves", n_moves), ("from_pool", from_pool),
+                                                      ("to_pool", to_pool), ("from_ksum", from_ksum), ("to_ksum", to_ksum),
+                                                      ("from_page2cluster", from_page2cluster),
+                                                      ("to_page2cluster", to_page2cluster))], src.numel(), 0)
+
+
+def swarm_move_pages_workspace_bytes(shape: swarm_shape) -> int:
+    n = int(load_library().swarm_move_pages_workspace_bytes(ctypes.byref(shape)))
+    if n < 0:
+        raise SwarmError(-n, "swarm_move_pages_workspace_bytes")
+    return n
+
+
+def swarm_move_pages(ctx, moves: swarm_page_moves, workspace: torch.Tensor, stream=None) -> None:
+    rc = load_library().swarm_move_pages(ctx, ctypes.byref(moves), _ptr(workspace, "workspace"),
+                                         ctypes.c_int64(workspace.numel() * workspace.element_size()), _stream(stream))
+    if rc != OK:
+        _check(rc, "swarm_move_pages", ctx)
+
+
+_LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def swarm_beam_select_workspace_bytes(batch: int, n_beams: int, vocab: int, n_keep: int) -> int:
+    n = int(load_library().swarm_beam_select_workspace_bytes(*[ctypes.c_int32(x) for x in (batch, n_beams, vocab, n_keep)]))
+    if n < 0:
+        raise SwarmError(-n, "swarm_beam_select_workspace_bytes")
+    return n
+
+
+def swarm_beam_select(logits: torch.Tensor, score: torch.Tensor, workspace: torch.Tensor, new_score: torch.Tensor,
+                      parent: torch.Tensor, token: torch.Tensor, stream=None) -> None:
+    """The best continuations of every prompt: logits [B, n_beams, vocab] (float32, bfloat16 or float16; rows may be padded),
+    score float32 [B, n_beams]; new_score (float32), parent and token (int32) [B, n_keep]."""
+    if logits.dtype not in _LOGIT_TYPES or logits.dim() != 3:
+        raise ValueError("logits must be a float32, bfloat16 or float16 tensor of three dimensions")
+    batch, beams, vocab = logits.shape
+    if not logits.is_cuda:
+        raise ValueError("logits must be a CUDA tensor")
+    pitch = logits.stride(1) if beams > 1 else logits.stride(0) if batch > 1 else vocab
+    if logits.stride(2) != 1 and vocab > 1 or pitch < vocab or (batch > 1 and logits.stride(0) != beams * pitch):
+        raise ValueError("logits must have contiguous rows at one distance")
+    keep = new_score.shape[-1]
+    _expect(score, "score", torch.float32, (batch, beams))
+    _expect(new_score, "new_score", torch.float32, (batch, keep))
+    _expect(parent, "parent", torch.int32, (batch, keep))
+    _expect(token, "token", torch.int32, (batch, keep))
+    rc = load_library().swarm_beam_select(ctypes.c_void_p(logits.data_ptr()), ctypes.c_int32(_LOGIT_TYPES[logits.dtype]),
+                                          ctypes.c_int64(pitch), _ptr(score, "score"), ctypes.c_int32(batch), ctypes.c_int32(beams),
+                                          ctypes.c_int32(vocab), ctypes.c_int32(keep), _ptr(workspace, "workspace"),
+                                          ctypes.c_int64(workspace.numel() * workspace.element_size()),
+                                          _ptr(new_score, "new_score"), _ptr(parent, "parent"), _ptr(token, "token"),
+                                          _stream(stream))
+    if rc != OK:
+        _check(rc, "swarm_beam_select")
 
 
 def swarm_device_status(ctx, stream=None) -> int:

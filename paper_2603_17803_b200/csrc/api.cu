@@ -320,6 +320,7 @@ int32_t swarm_create(const swarm_shape* shape, swarm_ctx** out_ctx) {
   if (e == cudaSuccess) e = configure_attention();
   if (e == cudaSuccess) e = configure_medoid();
   if (e == cudaSuccess) e = configure_tree();
+  if (e == cudaSuccess) e = configure_pages();
   if (e != cudaSuccess) {
     if (ctx->done_h != nullptr) cudaFreeHost(ctx->done_h);
     delete ctx;
@@ -903,6 +904,110 @@ int32_t swarm_tree_attn(swarm_ctx* ctx, const swarm_inputs* in, const swarm_tree
   c.lse = lse;
   SWARM_TRY(launch_tree_attn(ctx->geo, c, workspace, ws_ptr<uint32_t>(ctx, ctx->lay.status), static_cast<cudaStream_t>(stream)));
   return SWARM_OK;
+}
+
+int32_t swarm_append_tokens(swarm_ctx* ctx, const swarm_inputs* in, const swarm_new_tokens* t, void* kv_pool, void* ksum,
+                            int32_t* ctx_len_out, void* stream) {
+  SWARM_RANGE("swarm_append_tokens");
+  int32_t rc = need_ws(ctx);
+  if (rc != SWARM_OK) return rc;
+  if (in == nullptr || bad(in->page_base) || bad(in->ctx_len) || t == nullptr || bad(t->k) || bad(t->v) || bad(t->n_new) ||
+      !aligned16(t->path) || t->max_new < 1 || (t->path == nullptr ? t->max_path != 0 : t->max_path < 1) || bad(kv_pool) ||
+      !aligned16(ksum) || bad(ctx_len_out))
+    return SWARM_ERR_INVALID_ARG;
+  AppendCall c{};
+  c.k = static_cast<const uint16_t*>(t->k);
+  c.v = static_cast<const uint16_t*>(t->v);
+  c.path = t->path;
+  c.n_new = t->n_new;
+  c.T = t->max_new;
+  c.n_places = t->path != nullptr ? t->max_path : t->max_new;
+  c.page_base = in->page_base;
+  c.ctx_len = in->ctx_len;
+  c.kv_pool = static_cast<uint16_t*>(kv_pool);
+  c.ksum = static_cast<uint16_t*>(ksum);
+  c.ctx_len_out = ctx_len_out;
+  if (!append_supported(ctx->geo, c.n_places)) return SWARM_ERR_UNSUPPORTED;
+  SWARM_TRY(launch_append(ctx->geo, c, ws_ptr<unsigned>(ctx, ctx->lay.tickets), ws_ptr<uint32_t>(ctx, ctx->lay.status),
+                          static_cast<cudaStream_t>(stream)));
+  return SWARM_OK;
+}
+
+int32_t swarm_plan_pages(swarm_ctx* ctx, const swarm_page_plan* p, void* stream) {
+  SWARM_RANGE("swarm_plan_pages");
+  int32_t rc = need_ws(ctx);
+  if (rc != SWARM_OK) return rc;
+  if (p == nullptr || bad(p->page_base) || bad(p->ctx_len) || bad(p->parent) || !aligned16(p->reserve) || !aligned16(p->keep) ||
+      bad(p->new_page_base) || bad(p->new_ctx_len) || bad(p->src) || bad(p->dst) || bad(p->n_moves) || p->max_moves < 1 ||
+      p->new_page_base == p->page_base || p->new_ctx_len == p->ctx_len || (p->in_place != 0 && p->in_place != 1))
+    return SWARM_ERR_INVALID_ARG;
+  if (!pages_supported(ctx->geo)) return SWARM_ERR_UNSUPPORTED;
+  const PlanCall c{p->page_base, p->ctx_len, p->parent, p->reserve, p->keep, p->new_page_base, p->new_ctx_len, p->src, p->dst,
+                   p->n_moves, p->max_moves, p->in_place != 0};
+  SWARM_TRY(launch_plan_pages(ctx->geo, c, ws_ptr<uint32_t>(ctx, ctx->lay.status), static_cast<cudaStream_t>(stream)));
+  return SWARM_OK;
+}
+
+int64_t swarm_move_pages_workspace_bytes(const swarm_shape* shape) {
+  const int32_t rc = check_shape(shape);
+  if (rc != SWARM_OK) return -(int64_t)rc;
+  const Geometry g = geometry_of(*shape);
+  if (!pages_supported(g)) return -(int64_t)SWARM_ERR_UNSUPPORTED;
+  return move_pages_workspace_bytes(g);
+}
+
+int32_t swarm_move_pages(swarm_ctx* ctx, const swarm_page_moves* m, void* workspace, int64_t workspace_bytes, void* stream) {
+  SWARM_RANGE("swarm_move_pages");
+  int32_t rc = need_ws(ctx);
+  if (rc != SWARM_OK) return rc;
+  if (m == nullptr || bad(m->src) || bad(m->dst) || bad(m->n_moves) || bad(m->from_pool) || bad(m->to_pool) || !aligned16(m->from_ksum) ||
+      !aligned16(m->to_ksum) || !aligned16(m->from_page2cluster) || !aligned16(m->to_page2cluster) || m->max_moves < 1 || m->reserved != 0 ||
+      (m->from_ksum == nullptr) != (m->to_ksum == nullptr) || (m->from_page2cluster == nullptr) != (m->to_page2cluster == nullptr) ||
+      workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return SWARM_ERR_INVALID_ARG;
+  const Geometry& g = ctx->geo;
+  if (!pages_supported(g) || m->max_moves >= (1 << 30)) return SWARM_ERR_UNSUPPORTED;
+  if (workspace_bytes < move_pages_workspace_bytes(g)) return SWARM_ERR_WORKSPACE_TOO_SMALL;
+  // every table goes to itself, or to memory that does not overlap it
+  const bool in_place = m->from_pool == m->to_pool;
+  const int64_t sum_bytes = g.n_pool_pages * g.Hkv * 2 * kHeadDim * 2;
+  const struct { const void* from; const void* to; int64_t bytes; } tables[3] = {
+      {m->from_pool, m->to_pool, sum_bytes * g.S}, {m->from_ksum, m->to_ksum, sum_bytes}, {m->from_page2cluster, m->to_page2cluster, g.n_pool_pages * 4}};
+  for (const auto& t : tables) {
+    if (t.from == nullptr) continue;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(t.from), b = reinterpret_cast<uintptr_t>(t.to);
+    if (in_place ? a != b : (a < b + t.bytes && b < a + t.bytes)) return SWARM_ERR_INVALID_ARG;
+  }
+  const MoveCall c{m->src, m->dst, m->n_moves, m->max_moves, in_place, m->from_pool, m->to_pool, m->from_ksum, m->to_ksum,
+                   m->from_page2cluster, m->to_page2cluster};
+  SWARM_TRY(launch_move_pages(g, c, workspace, ws_ptr<uint32_t>(ctx, ctx->lay.status), static_cast<cudaStream_t>(stream)));
+  return SWARM_OK;
+}
+
+namespace {
+int32_t check_beams(int32_t batch, int32_t n_beams, int32_t vocab, int32_t n_keep) {
+  if (batch < 1 || n_beams < 1 || vocab < 1 || n_keep < 1) return SWARM_ERR_INVALID_ARG;
+  return n_keep <= kMaxBeamKeep && beam_supported(batch, n_beams, vocab, n_keep) ? SWARM_OK : SWARM_ERR_UNSUPPORTED;
+}
+}  // namespace
+
+int64_t swarm_beam_select_workspace_bytes(int32_t batch, int32_t n_beams, int32_t vocab, int32_t n_keep) {
+  const int32_t rc = check_beams(batch, n_beams, vocab, n_keep);
+  return rc != SWARM_OK ? -(int64_t)rc : beam_select_workspace_bytes(batch, n_beams, vocab, n_keep);
+}
+
+int32_t swarm_beam_select(const void* logits, int32_t dtype, int64_t row_stride, const float* score, int32_t batch, int32_t n_beams,
+                          int32_t vocab, int32_t n_keep, void* workspace, int64_t workspace_bytes, float* new_score,
+                          int32_t* parent, int32_t* token, void* stream) {
+  SWARM_RANGE("swarm_beam_select");
+  if (bad(logits) || dtype < SWARM_DTYPE_F32 || dtype > SWARM_DTYPE_F16 || row_stride < vocab || bad(score) || bad(workspace) ||
+      bad(new_score) || bad(parent) || bad(token))
+    return SWARM_ERR_INVALID_ARG;
+  const int32_t rc = check_beams(batch, n_beams, vocab, n_keep);
+  if (rc != SWARM_OK) return rc;
+  if (workspace_bytes < beam_select_workspace_bytes(batch, n_beams, vocab, n_keep)) return SWARM_ERR_WORKSPACE_TOO_SMALL;
+  const BeamCall c{logits, dtype, row_stride, score, batch, n_beams, vocab, n_keep, new_score, parent, token};
+  return launch_beam_select(c, workspace, static_cast<cudaStream_t>(stream)) == cudaSuccess ? SWARM_OK : SWARM_ERR_CUDA;
 }
 
 int32_t swarm_step_host(swarm_ctx* ctx, const swarm_inputs* in, const swarm_outputs* o, const void* q_host,

@@ -318,6 +318,72 @@ long long tree_attn_workspace_bytes(const Geometry& geo, int T);
 cudaError_t configure_tree();
 cudaError_t launch_tree_attn(const Geometry& geo, const TreeCall& c, void* workspace, uint32_t* status, cudaStream_t st);
 
+// New tokens written to the cache: see append.cu.
+struct AppendCall {
+  const uint16_t* k;
+  const uint16_t* v;
+  const int32_t* path;      // [B][n_places] or null
+  const int32_t* n_new;
+  int T, n_places;
+  const int64_t* page_base;
+  const int32_t* ctx_len;
+  uint16_t* kv_pool;
+  uint16_t* ksum;
+  int32_t* ctx_len_out;
+};
+bool append_supported(const Geometry& geo, int n_places);
+cudaError_t launch_append(const Geometry& geo, const AppendCall& c, unsigned* tickets, uint32_t* status, cudaStream_t st);
+
+// Re-layout of the cache: see pages.cu.
+struct PlanCall {
+  const int64_t* page_base;
+  const int32_t* ctx_len;
+  const int32_t* parent;
+  const int32_t* reserve;
+  const uint8_t* keep;
+  int64_t* new_page_base;
+  int32_t* new_ctx_len;
+  int32_t* src;
+  int32_t* dst;
+  int32_t* n_moves;
+  int max_moves;
+  bool in_place;
+};
+struct MoveCall {
+  const int32_t* src;
+  const int32_t* dst;
+  const int32_t* n_moves;
+  int max_moves;
+  bool in_place;
+  const void* from_pool;
+  void* to_pool;
+  const void* from_ksum;
+  void* to_ksum;
+  const int32_t* from_p2c;
+  int32_t* to_p2c;
+};
+cudaError_t configure_pages();
+bool pages_supported(const Geometry& geo);
+long long move_pages_workspace_bytes(const Geometry& geo);
+cudaError_t launch_plan_pages(const Geometry& geo, const PlanCall& c, uint32_t* status, cudaStream_t st);
+cudaError_t launch_move_pages(const Geometry& geo, const MoveCall& c, void* workspace, uint32_t* status, cudaStream_t st);
+
+// Beam search's selection: see beam.cu.
+constexpr int kMaxBeamKeep = 64;
+struct BeamCall {
+  const void* logits;
+  int dtype;
+  long long row_stride;     // elements between the rows of consecutive beams
+  const float* score;
+  int batch, n_beams, vocab, n_keep;
+  float* new_score;
+  int32_t* parent;
+  int32_t* token;
+};
+bool beam_supported(int batch, int n_beams, int vocab, int n_keep);
+long long beam_select_workspace_bytes(int batch, int n_beams, int vocab, int n_keep);
+cudaError_t launch_beam_select(const BeamCall& c, void* workspace, cudaStream_t st);
+
 // Algorithm 1 (offline co-activation clustering): see cluster.cu.
 long long build_clusters_workspace_bytes(int n);
 cudaError_t launch_build_clusters(const float* dist, int n, float tau, void* workspace, int32_t* rho, int32_t* ptr,
