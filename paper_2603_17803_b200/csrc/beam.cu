@@ -2,13 +2,15 @@
 //   score[beam] + logit[beam][token] - log sum_v exp(logit[beam][v]),
 // ties to the lowest beam * vocab + token.
 //
-// First kernel, a CTA per chunk of a beam's row: the chunk lives in registers, read once; its maximum and sum of
-// exponentials, and its n_keep largest logits.  (Inside a row the order of the sums is the order of the logits.)  Second
-// kernel, a CTA per prompt: log-sum-exp of every beam and the n_keep best of all chunks' candidates, in 64 bits, since
-// candidates of different beams may differ by less than fp32 holds.
+// First kernel, a CTA per stretch of a beam's row, which it reads once, a chunk in registers at a time: a running maximum and sum
+// of exponentials per thread, joined at the end, and the n_keep largest logits so far.  (Inside a row the order of the sums is the
+// order of the logits.)  Second kernel, a CTA per prompt: log-sum-exp of every beam and the n_keep best of all stretches'
+// candidates, in 64 bits, since candidates of different beams may differ by less than fp32 holds.
 //
-// The n_keep largest of a chunk: the n_keep-th largest of the threads' own maxima is a lower bound of the n_keep-th largest
-// element, and only the n_keep threads above it can hold candidates; those few are gathered and ranked by counting.
+// The n_keep largest: once n_keep logits are held, only those above the least of them matter, and soon hardly any thread has
+// one.  In a chunk where many threads do (the first one), the n_keep-th largest of the maxima of groups of threads is a lower
+// bound of what can be chosen, and only the n_keep groups above it can hold candidates; those few are gathered and ranked
+// by counting.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -30,14 +32,9 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
-__device__ __forceinline__ key_t make_key(float x, uint32_t index) { return ((key_t)ordered(x) << 32) | (uint32_t)~index; }
+__device__ __forceinline__ key_t make_key(float x, uint32_t index) { return ((key_t)ordered(x + 0.f) << 32) | (uint32_t)~index; }   // (-0 as 0)
 __device__ __forceinline__ uint32_t key_index(key_t k) { return ~(uint32_t)k; }
 __device__ __forceinline__ float key_value(key_t k) { return unordered((uint32_t)(k >> 32)); }
-__device__ __forceinline__ float exp_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * kLog2e));
-  return y;
-}
 
 template <class T> struct Element;
 template <> struct Element<float> {
@@ -67,47 +64,48 @@ template <> struct Element<__half> {
   }
 };
 
-// Per thread kPer elements of a chunk of kBeamThreads * kPer; `chunks` of them cover a row.
+// 2^(t * log2 e) for t <= 0, the constant in two parts: the sums of different beams are compared far below 2^-24 of the exponent.
+__device__ __forceinline__ float exp_fast(float t) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaf(t, 1.9259629911e-8f, t * kLog2e)));
+  return y;
+}
+
+// A chunk is kPer tokens for each of kBeamThreads threads; a CTA takes `span` chunks of a row one after the other.
 template <class T, int kPer>
-__global__ void __launch_bounds__(kBeamThreads)
-beam_chunk_kernel(const BeamCall c, int chunks, key_t* __restrict__ keys, float2* __restrict__ sums) {
-  constexpr int kVec = 16 / (int)sizeof(T), kVecs = kPer / kVec;
-  __shared__ key_t s_max[kBeamThreads];
-  __shared__ key_t s_cand[64 * kPer];
-  __shared__ float s_red[2][kBeamThreads / 32];
+__global__ void __launch_bounds__(kBeamThreads, kPer == 32 ? 3 : 4)
+beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__ keys, float2* __restrict__ sums) {
+  constexpr int kVec = 16 / (int)sizeof(T), kVecs = kPer / kVec, kChunk = kBeamThreads * kPer;
+  constexpr int kMany = 64;                                   // threads with a candidate that are gathered as they are
+  __shared__ key_t s_max[128];
+  __shared__ key_t s_cand[kMaxBeamKeep + 128 * kPer];
+  __shared__ key_t s_top[kMaxBeamKeep];
+  __shared__ float2 s_red[kBeamThreads / 32];
   __shared__ key_t s_bound;
   __shared__ int s_count;
   pdl_wait();
   pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int row = blockIdx.x / chunks, chunk = blockIdx.x - row * chunks;
+  const int row = blockIdx.x / stretches, stretch = blockIdx.x - row * stretches;
   const int V = c.vocab, keep = c.n_keep;
   // Rows may start anywhere in a 16-byte line.  The tokens a thread has do not depend on that (equal rows give equal sums, and so
   // ties between beams stay ties): a vector across two lines is put together from both.
   const char* first = static_cast<const char*>(c.logits) + (long long)row * c.row_stride * (int)sizeof(T);
   const char* end = static_cast<const char*>(c.logits) + ((long long)(c.batch * c.n_beams - 1) * c.row_stride + V) * (int)sizeof(T);
   const int shift = (int)(reinterpret_cast<uintptr_t>(first) & 15u);
-  float x[kPer];
-  uint4 lo[kVecs], hi[kVecs];
-  const int at0 = chunk * kBeamThreads * kPer;
-  auto whole = [&](int at) { return at < V && first + (long long)at * (int)sizeof(T) + (shift ? 32 - shift : 16) <= end; };
+  auto whole = [&](int at) { return at + kVec <= V && first + (long long)at * (int)sizeof(T) + (shift ? 32 - shift : 16) <= end; };
+  uint4 raw[kVecs];
+  auto fetch = [&](int at0) {
 #pragma unroll
-  for (int i = 0; i < kVecs; ++i) {
-    const int at = at0 + (i * kBeamThreads + tid) * kVec;
-    if (whole(at)) {
+    for (int i = 0; i < kVecs; ++i) {
+      const int at = at0 + (i * kBeamThreads + tid) * kVec;
+      if (!whole(at)) continue;
       const char* p = first + (long long)at * (int)sizeof(T) - shift;
-      lo[i] = shift ? __ldg(reinterpret_cast<const uint4*>(p)) : ldg_nc_v4(p);
-      if (shift) hi[i] = __ldg(reinterpret_cast<const uint4*>(p + 16));
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kVecs; ++i) {
-    const int at = at0 + (i * kBeamThreads + tid) * kVec;
-    const bool full = whole(at);
-    if (full) {
-      uint4 v = lo[i];
-      if (shift) {
-        uint32_t w[8] = {lo[i].x, lo[i].y, lo[i].z, lo[i].w, hi[i].x, hi[i].y, hi[i].z, hi[i].w};
+      if (shift == 0) {
+        raw[i] = ldg_nc_v4(p);
+      } else {
+        const uint4 lo = __ldg(reinterpret_cast<const uint4*>(p)), hi = __ldg(reinterpret_cast<const uint4*>(p + 16));
+        uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
         if (shift & 4) {
 #pragma unroll
           for (int z = 0; z < 7; ++z) w[z] = w[z + 1];
@@ -117,77 +115,131 @@ beam_chunk_kernel(const BeamCall c, int chunks, key_t* __restrict__ keys, float2
           for (int z = 0; z < 5; ++z) w[z] = w[z + 2];
         }
         const int bits = (shift & 3) * 8;
-        v = make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
-                       __funnelshift_r(w[3], w[4], bits));
+        raw[i] = make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                            __funnelshift_r(w[3], w[4], bits));
       }
-      Element<T>::unpack(v, x + i * kVec);
     }
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-      float& f = x[i * kVec + e];
-      if (at + e >= V) f = -INFINITY;
-      else if (!full) f = Element<T>::one(first, at + e);
-      if (!(f == f)) f = -INFINITY;                           // NaN: never chosen
-    }
-  }
-  // the thread's largest, the first of equal ones
-  float mine = -INFINITY;
-  int where = 0;
-#pragma unroll
-  for (int e = 0; e < kPer; ++e)
-    if (x[e] > mine) { mine = x[e]; where = e; }
-  auto token = [&](int e) { return at0 + ((e / kVec) * kBeamThreads + tid) * kVec + e % kVec; };
-  s_max[tid] = make_key(mine, (uint32_t)token(where));
-  float top = mine;
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-  if (lane == 0) s_red[0][warp] = top;
+  };
+  const int begin = stretch * span * kChunk, stop = min(V, begin + span * kChunk);
   if (tid == 0) s_count = 0;
-  __syncthreads();
-  top = s_red[0][0];
+  float top = -INFINITY, sum = 0.f;                           // of this thread's logits so far
+  float floor_ = -INFINITY;                                   // the least of the n_keep held, once there are as many
+  fetch(begin);
+  for (int at0 = begin; at0 < stop; at0 += kChunk) {
+    float x[kPer];
 #pragma unroll
-  for (int w = 1; w < kBeamThreads / 32; ++w) top = fmaxf(top, s_red[0][w]);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float sum[2] = {0.f, 0.f};
+    for (int i = 0; i < kVecs; ++i) {
+      const int at = at0 + (i * kBeamThreads + tid) * kVec;
+      if (whole(at)) {
+        Element<T>::unpack(raw[i], x + i * kVec);
+      } else {
 #pragma unroll
-  for (int e = 0; e < kPer; ++e) sum[e & 1] += exp_fast(x[e] - ref);
-  float all = sum[0] + sum[1];
-#pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
-  if (lane == 0) s_red[1][warp] = all;
-  // the n_keep-th largest of the threads' maxima
-  int above = 0;
-  const key_t my_key = s_max[tid];
-#pragma unroll 8
-  for (int i = 0; i < kBeamThreads; i += 2) {
-    const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(s_max + i);
-    above += (two.x > my_key) + (two.y > my_key);
-  }
-  if (above == keep - 1) s_bound = my_key;
-  __syncthreads();
-  const key_t bound = s_bound;
-  if (my_key >= bound) {
+        for (int e = 0; e < kVec; ++e) x[i * kVec + e] = at + e < V ? Element<T>::one(first, at + e) : -INFINITY;
+      }
+    }
+    if (at0 + kChunk < stop) fetch(at0 + kChunk);             // the next chunk is on its way meanwhile
+    float mine = -INFINITY;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
-      const key_t k = make_key(x[e], (uint32_t)token(e));
-      if (k >= bound && x[e] != -INFINITY) s_cand[atomicAdd(&s_count, 1)] = k;
+      x[e] = fmaxf(x[e], -INFINITY);                          // NaN: never chosen
+      mine = fmaxf(mine, x[e]);
+    }
+    if (mine > top) {
+      sum *= exp_fast(top - mine);                            // (0 * 2^-inf the first time)
+      top = mine;
+    }
+    const float ref = top == -INFINITY ? 0.f : top;
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) part[e & 3] += exp_fast(x[e] - ref);
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
+
+    const bool hit = mine > floor_;
+    const int hits = __syncthreads_count(hit);
+    if (hits == 0) continue;
+    auto token = [&](int e) { return (uint32_t)(at0 + ((e / kVec) * kBeamThreads + tid) * kVec + e % kVec); };
+    key_t bound = 0;
+    float bound_value = -INFINITY;
+    if (hits > kMany) {
+      const int group = keep > 32 ? 2 : 4, groups = kBeamThreads / group;
+      int where = 0;
+#pragma unroll
+      for (int e = kPer - 1; e >= 0; --e)
+        if (x[e] == mine) where = e;                          // the first of equal ones
+      key_t best = make_key(mine, token(where));
+      for (int o = 1; o < group; o <<= 1) {
+        const key_t other = __shfl_xor_sync(0xFFFFFFFFu, best, o);
+        if (other > best) best = other;
+      }
+      if (tid % group == 0) s_max[tid / group] = best;
+      __syncthreads();
+      if (tid < groups) {
+        const key_t my_key = s_max[tid];
+        int above = 0;
+#pragma unroll 8
+        for (int i = 0; i < groups; i += 2) {
+          const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(s_max + i);
+          above += (two.x > my_key) + (two.y > my_key);
+        }
+        if (above == keep - 1) s_bound = my_key;
+      }
+      __syncthreads();
+      bound = s_bound;
+      bound_value = key_value(bound);
+    }
+    if (hit && mine >= bound_value) {
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        if (x[e] > floor_) {
+          const key_t k = make_key(x[e], token(e));
+          if (k >= bound) s_cand[atomicAdd(&s_count, 1)] = k;
+        }
+      }
+    }
+    __syncthreads();
+    const int n = s_count;
+    if (n < keep) continue;                                   // (the next writes are behind the next barrier)
+    for (int i = tid; i < n; i += kBeamThreads) {
+      const key_t k = s_cand[i];
+      int rank = 0;
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) rank += s_cand[j] > k;
+      if (rank < keep) s_top[rank] = k;
+    }
+    __syncthreads();
+    if (tid < keep) s_cand[tid] = s_top[tid];
+    if (tid == 0) s_count = keep;
+    floor_ = key_value(s_top[keep - 1]);
+  }
+  // the threads' sums
+  float m = top;
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+  float l = top == -INFINITY ? 0.f : sum * exp_fast(top - m);
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+  if (lane == 0) s_red[warp] = make_float2(m, l);
+  __syncthreads();
+  key_t* out = keys + (long long)blockIdx.x * keep;
+  const int n = s_count;                                      // at most n_keep, in no order while fewer
+  if (tid < keep) {
+    if (tid < n) {
+      const key_t k = s_cand[tid];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += s_cand[j] > k;
+      out[rank] = k;
+    } else {
+      out[tid] = 0;                                           // no such candidate (below the key of every logit)
     }
   }
-  __syncthreads();
-  const int n = s_count;
-  key_t* out = keys + (long long)blockIdx.x * keep;
-  for (int i = tid; i < n; i += kBeamThreads) {
-    const key_t k = s_cand[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += s_cand[j] > k;
-    if (rank < keep) out[rank] = k;
-  }
-  for (int i = n + tid; i < keep; i += kBeamThreads) out[i] = 0;   // no such candidate (below the key of every logit)
   if (tid == 0) {
-    float l = 0.f;
+    float M = -INFINITY, all = 0.f;
 #pragma unroll
-    for (int w = 0; w < kBeamThreads / 32; ++w) l += s_red[1][w];
-    sums[blockIdx.x] = make_float2(top, l);
+    for (int w = 0; w < kBeamThreads / 32; ++w) M = fmaxf(M, s_red[w].x);
+#pragma unroll
+    for (int w = 0; w < kBeamThreads / 32; ++w)
+      if (s_red[w].x != -INFINITY) all += s_red[w].y * exp_fast(s_red[w].x - M);
+    sums[blockIdx.x] = make_float2(M, all);
   }
 }
 
@@ -238,7 +290,7 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
     const int beam = i / per_beam;
     Cand r;
     const double s = (double)c.score[b * c.n_beams + beam] + ((double)key_value(k) - s_base[beam]);
-    r.value = k == 0 || !(s > -INFINITY) ? 0 : ordered(s);
+    r.value = k == 0 || !(s > -INFINITY) ? 0 : ordered(s + 0.0);
     r.index = (uint32_t)beam * (uint32_t)V + key_index(k);
     return r;
   };
@@ -289,10 +341,19 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
   }
 }
 
-// Elements per thread: a chunk is kBeamThreads times as many.  16 for few rows of small vocabularies (more CTAs, shorter
-// ones), 32 otherwise.
-int per_thread(long long rows, int vocab) { return rows * ((vocab + 8191) / 8192) < 296 ? 16 : 32; }
-int chunks_of(int vocab, int per) { return (vocab + kBeamThreads * per - 1) / (kBeamThreads * per); }
+// How a row is cut.  Elements per thread: 64 bytes of them (with the next 64 on their way), of 16-bit types 32 bytes where that
+// leaves SMs without a chunk.  Chunks per CTA: the first is the dear one, but about twelve CTAs per SM even out the waves.
+struct Cut {
+  int per, span, stretches;
+};
+Cut cut_of(long long rows, int vocab, int dtype) {
+  Cut c;
+  auto chunks = [&](int per) { return (vocab + kBeamThreads * per - 1) / (kBeamThreads * per); };
+  c.per = dtype == SWARM_DTYPE_F32 || rows * chunks(32) < 148 ? 16 : 32;
+  c.span = (int)std::max<long long>(1, std::min<long long>(32, rows * chunks(c.per) / (148 * 12)));
+  c.stretches = (chunks(c.per) + c.span - 1) / c.span;
+  return c;
+}
 constexpr int kMergeSmemMax = 200 * 1024;
 // Shared memory of the second kernel: every thread of the n_keep groups above the bound may bring all of its candidates.
 long long merge_smem(int beams, int chunks, int keep, int group) {
@@ -302,42 +363,48 @@ long long merge_smem(int beams, int chunks, int keep, int group) {
 int merge_group(int beams, int chunks, int keep) { return merge_smem(beams, chunks, keep, 4) <= kMergeSmemMax ? 4 : 1; }
 
 template <class T>
-cudaError_t launch_chunks(const BeamCall& c, int per, int chunks, key_t* keys, float2* sums, cudaStream_t st) {
-  const dim3 grid((unsigned)((long long)c.batch * c.n_beams * chunks));
-  return per == 16 ? launch_pdl(beam_chunk_kernel<T, 16>, grid, dim3(kBeamThreads), 0, st, true, c, chunks, keys, sums)
-                   : launch_pdl(beam_chunk_kernel<T, 32>, grid, dim3(kBeamThreads), 0, st, true, c, chunks, keys, sums);
+cudaError_t launch_chunks(const BeamCall& c, const Cut& cut, key_t* keys, float2* sums, cudaStream_t st) {
+  const dim3 grid((unsigned)((long long)c.batch * c.n_beams * cut.stretches));
+  if constexpr (sizeof(T) == 2)
+    if (cut.per == 32)
+      return launch_pdl(beam_chunk_kernel<T, 32>, grid, dim3(kBeamThreads), 0, st, true, c, cut.stretches, cut.span, keys, sums);
+  return launch_pdl(beam_chunk_kernel<T, 16>, grid, dim3(kBeamThreads), 0, st, true, c, cut.stretches, cut.span, keys, sums);
 }
 
 constexpr int64_t align256(int64_t x) { return (x + 255) & ~int64_t(255); }
 
+// (Whatever the type of the logits: 16 elements per thread give the most stretches.)
+int most_stretches(long long rows, int vocab) {
+  return std::max(cut_of(rows, vocab, SWARM_DTYPE_F32).stretches, cut_of(rows, vocab, SWARM_DTYPE_BF16).stretches);
+}
 }  // namespace
 
 bool beam_supported(int batch, int n_beams, int vocab, int n_keep) {
   const long long rows = (long long)batch * n_beams;
-  const int per = per_thread(rows, vocab), chunks = chunks_of(vocab, per);
-  return (long long)n_beams * vocab < (1LL << 31) && rows * chunks < (1LL << 31) && (long long)n_beams * chunks * n_keep < (1LL << 30) &&
-         merge_smem(n_beams, chunks, n_keep, 1) <= kMergeSmemMax;
+  const int parts = most_stretches(rows, vocab);
+  return (long long)n_beams * vocab < (1LL << 31) && rows * parts < (1LL << 31) && (long long)n_beams * parts * n_keep < (1LL << 30) &&
+         merge_smem(n_beams, parts, n_keep, 1) <= kMergeSmemMax;
 }
 
 long long beam_select_workspace_bytes(int batch, int n_beams, int vocab, int n_keep) {
-  const long long rows = (long long)batch * n_beams, chunks = chunks_of(vocab, per_thread(rows, vocab));
-  return align256(rows * chunks * n_keep * 8) + align256(rows * chunks * 8);
+  const long long rows = (long long)batch * n_beams, parts = most_stretches(rows, vocab);
+  return align256(rows * parts * n_keep * 8) + align256(rows * parts * 8);
 }
 
 cudaError_t launch_beam_select(const BeamCall& c, void* workspace, cudaStream_t st) {
   const long long rows = (long long)c.batch * c.n_beams;
-  const int per = per_thread(rows, c.vocab), chunks = chunks_of(c.vocab, per);
+  const Cut cut = cut_of(rows, c.vocab, c.dtype);
   key_t* keys = static_cast<key_t*>(workspace);
-  float2* sums = reinterpret_cast<float2*>(static_cast<unsigned char*>(workspace) + align256(rows * chunks * c.n_keep * 8));
-  const int group = merge_group(c.n_beams, chunks, c.n_keep);
-  const size_t smem = (size_t)merge_smem(c.n_beams, chunks, c.n_keep, group);
+  float2* sums = reinterpret_cast<float2*>(static_cast<unsigned char*>(workspace) + align256(rows * cut.stretches * c.n_keep * 8));
+  const int group = merge_group(c.n_beams, cut.stretches, c.n_keep);
+  const size_t smem = (size_t)merge_smem(c.n_beams, cut.stretches, c.n_keep, group);
   cudaError_t e = cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMergeSmemMax);
   if (e != cudaSuccess) return e;
-  e = c.dtype == SWARM_DTYPE_F32    ? launch_chunks<float>(c, per, chunks, keys, sums, st)
-      : c.dtype == SWARM_DTYPE_BF16 ? launch_chunks<__nv_bfloat16>(c, per, chunks, keys, sums, st)
-                                    : launch_chunks<__half>(c, per, chunks, keys, sums, st);
+  e = c.dtype == SWARM_DTYPE_F32    ? launch_chunks<float>(c, cut, keys, sums, st)
+      : c.dtype == SWARM_DTYPE_BF16 ? launch_chunks<__nv_bfloat16>(c, cut, keys, sums, st)
+                                    : launch_chunks<__half>(c, cut, keys, sums, st);
   if (e != cudaSuccess) return e;
-  return launch_pdl(beam_merge_kernel, dim3((unsigned)c.batch), dim3(kMergeThreads), smem, st, true, c, chunks, group, keys, sums);
+  return launch_pdl(beam_merge_kernel, dim3((unsigned)c.batch), dim3(kMergeThreads), smem, st, true, c, cut.stretches, group, keys, sums);
 }
 
 }  // namespace swarm
