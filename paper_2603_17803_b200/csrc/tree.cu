@@ -8,6 +8,7 @@
 //
 //   warps 0-3, 4-7   two softmax streams, a thread per row of 128 (tcgen05.ld: lane = row)
 //   warp 8           copies: K and V tiles of 32 KB by TMA into a ring, 128-byte swizzle
+//   warp 11          lists the CTA's share of the work (warp 10 only fills the warpgroup, whose registers go to the softmax)
 //   warp 9           matrix products: S = Q K^T (operands in shared memory), O += P V (P from tensor memory)
 // Tensor memory: S0, S1 (128 columns each; P, in bf16, takes the place of S), O0, O1.  While one stream is in its softmax
 // the tensor core works for the other.  Up to 128 rows: the streams take alternate tiles of the same rows, and their
@@ -19,6 +20,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "swarm_internal.cuh"
 
@@ -28,7 +30,7 @@ namespace {
 constexpr int kTile = 128;                                 // tokens of a tile, rows of a stream
 constexpr int kTileBytes = kTile * kHeadDim * 2;           // K or V of a tile: two halves of 64 coordinates
 constexpr int kHalfBytes = kTileBytes / 2;
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;
 constexpr int kSegs = 32;                                  // segments of a CTA listed at a time
 constexpr int kMaxTreeCtas = 148;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -112,14 +114,16 @@ __device__ __forceinline__ void tmem_ld32(uint32_t (&r)[32], uint32_t addr) {
         "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr));
 }
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t addr) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
-      "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
-      "r"(r[31])
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -153,10 +157,64 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
       "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
       : "memory");
 }
+// True in one lane of the warp.  With a condition on the lane's number instead, the operands of a product are not known to be
+// uniform and move to uniform registers one by one: 100 cycles to issue each.
+__device__ __forceinline__ bool one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
 __device__ __forceinline__ float exp2_fast(float x) {      // 2^x, relative error about 2^-22; 0 for x = -inf
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// Two floats in a register pair: one instruction for both.
+typedef unsigned long long pair_t;
+__device__ __forceinline__ pair_t pair_of(float lo, float hi) {
+  pair_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair(pair_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ pair_t fma2(pair_t a, pair_t b, pair_t c) {
+  pair_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ pair_t add2(pair_t a, pair_t b) {
+  pair_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 2^y of both for y > -126: y = n + f with n whole and |f| <= 1/2, 2^f by a polynomial of degree 5 (fitted to the least largest
+// relative error, 2.1e-7 in fp32), n added to the exponent.  It runs on the multiply-add units, beside the exponentials of the
+// special function unit (kByFma: which pairs of eight), which a tile of 256 rows would keep busy for longer than its K and V
+// take to arrive.
+constexpr unsigned kByFma = 0x52u;
+__device__ __forceinline__ void exp2_pair(pair_t y, float& lo, float& hi) {
+  float y0, y1;
+  unpair(y, y0, y1);
+  y = pair_of(fmaxf(y0, -125.f), fmaxf(y1, -125.f));
+  const pair_t magic = pair_of(12582912.f, 12582912.f), n = add2(y, magic);   // 1.5 * 2^23: the whole part ends in the low bits
+  const pair_t f = fma2(add2(n, pair_of(-12582912.f, -12582912.f)), pair_of(-1.f, -1.f), y);
+  pair_t r = pair_of(0.0013276466634124517f, 0.0013276466634124517f);
+  r = fma2(r, f, pair_of(0.009675540961325169f, 0.009675540961325169f));
+  r = fma2(r, f, pair_of(0.05550713464617729f, 0.05550713464617729f));
+  r = fma2(r, f, pair_of(0.24022120237350464f, 0.24022120237350464f));
+  r = fma2(r, f, pair_of(0.6931469440460205f, 0.6931469440460205f));
+  r = fma2(r, f, pair_of(1.0000001192092896f, 1.0000001192092896f));
+  float r0, r1, n0, n1;
+  unpair(r, r0, r1);
+  unpair(n, n0, n1);
+  lo = __uint_as_float(__float_as_uint(r0) + (__float_as_uint(n0) << 23));
+  hi = __uint_as_float(__float_as_uint(r1) + (__float_as_uint(n1) << 23));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
 struct TreeArgs {
@@ -214,7 +272,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
   float2* ml = reinterpret_cast<float2*>(smem + L::kMl);     // [2][128] of the two streams
   long long* scan = reinterpret_cast<long long*>(smem + L::kScan);
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);    // (known to be the same for the whole warp: see `one`)
   const int rb = blockIdx.x % a.row_blocks, chunk = blockIdx.x / a.row_blocks;
   const int g = a.geo.g, Hkv = a.geo.Hkv, S = a.geo.S;
   const int units = a.geo.B * Hkv;
@@ -274,8 +333,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
       if (at + n > w0) break;
       at += n;
     }
-    scan[12] = u;
-    scan[13] = at;
+    scan[kThreads / 32] = u;
+    scan[kThreads / 32 + 1] = at;
   }
   __syncthreads();
   const uint32_t tmem = *tmem_at;
@@ -287,54 +346,63 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
   int issued = 0;                                            // copies started (producer)
   bool ok = true;
   bool first_list = true;
-  int u_next = w0 < w1 ? (int)scan[12] : units;
-  long long at_next = w0 < w1 ? scan[13] : 0;
+  int u_next = w0 < w1 ? (int)scan[kThreads / 32] : units;
+  long long at_next = w0 < w1 ? scan[kThreads / 32 + 1] : 0;
 
-  while (u_next < units && at_next < w1) {
-    // ---- the next (up to 32) units with tiles in this CTA's share
-    __syncthreads();                                         // the previous list has been worked through
-    if (warp == 0) {
-      const int u = u_next + lane;
-      int ctx = 0, nd = 0, n = 0;
-      bool bad;
-      if (u < units) {
-        unit_lengths(a, u, ctx, nd, bad);
-        n = tiles_of(ctx, nd);
-      }
-      long long end = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xFFFFFFFFu, end, o);
-        if (lane >= o) end += v;
-      }
-      end += at_next;
-      const long long begin = end - n;
-      const bool here = n > 0 && begin < w1 && end > w0;
-      const unsigned all = __ballot_sync(0xFFFFFFFFu, here);
-      if (here) {
-        Seg s;
-        s.b = u / Hkv;
-        s.kv = u - s.b * Hkv;
-        s.t0 = (int)(max(w0, begin) - begin);
-        s.t1 = (int)(min(w1, end) - begin);
-        s.ctx_tiles = (ctx + kTile - 1) / kTile;
-        s.ctx_tokens = ctx;
-        s.nd = nd;
-        s.last = s.t1 == n;
-        list[__popc(all & ((1u << lane) - 1u))] = s;
-        if (rb == 0) {
-          if (s.t0 == 0) a.unit_first[u] = 2 * chunk + (begin == w0 ? 0 : 1);
-          if (s.last) a.unit_last[u] = chunk;
+  int count = 0;
+  // Calls `work` for one list of segments after the other; every warp of the CTA goes through the same lists.
+  auto lists = [&](auto&& work) {
+    while (u_next < units && at_next < w1) {
+      __syncthreads();                                       // the previous list has been worked through
+      if (*stop != 0) break;
+      if (warp == 11) {                                      // the next (up to 32) units with tiles in this CTA's share
+        const int u = u_next + lane;
+        int ctx = 0, nd = 0, n = 0;
+        bool bad;
+        if (u < units) {
+          unit_lengths(a, u, ctx, nd, bad);
+          n = tiles_of(ctx, nd);
         }
+        long long end = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const long long v = __shfl_up_sync(0xFFFFFFFFu, end, o);
+          if (lane >= o) end += v;
+        }
+        end += at_next;
+        const long long begin = end - n;
+        const bool here = n > 0 && begin < w1 && end > w0;
+        const unsigned all = __ballot_sync(0xFFFFFFFFu, here);
+        if (here) {
+          Seg s;
+          s.b = u / Hkv;
+          s.kv = u - s.b * Hkv;
+          s.t0 = (int)(max(w0, begin) - begin);
+          s.t1 = (int)(min(w1, end) - begin);
+          s.ctx_tiles = (ctx + kTile - 1) / kTile;
+          s.ctx_tokens = ctx;
+          s.nd = nd;
+          s.last = s.t1 == n;
+          list[__popc(all & ((1u << lane) - 1u))] = s;
+          if (rb == 0) {
+            if (s.t0 == 0) a.unit_first[u] = 2 * chunk + (begin == w0 ? 0 : 1);
+            if (s.last) a.unit_last[u] = chunk;
+          }
+        }
+        if (lane == 31) scan[kThreads / 32 + 2] = end;
+        if (lane == 0) *n_segs = __popc(all);
       }
-      if (lane == 31) scan[14] = end;
-      if (lane == 0) *n_segs = __popc(all);
+      __syncthreads();
+      count = *n_segs;
+      u_next += 32;
+      at_next = scan[kThreads / 32 + 2];
+      work();
+      first_list = false;
     }
-    __syncthreads();
-    const int count = *n_segs;
-    u_next += 32;
-    at_next = scan[14];
+  };
 
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");     // 128 * 72 + 256 * 216 = 384 * 168, what the CTA was launched with
     if (warp == 8) {
       // ---- copies, in the order the matrix products use them
       auto load_tile = [&](const Seg& s, int t, int which) -> bool {   // which: 0 = K, 1 = V
@@ -366,6 +434,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         if (++slot == L::kSlots) { slot = 0; ring_phase ^= 1u; }
         return true;
       };
+      lists([&] {
       for (int i = 0; ok && i < count; ++i) {
         const Seg s = list[i];
         if (rb * L::kRows >= s.nd * g) continue;
@@ -385,6 +454,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
           }
         }
       }
+      });
     } else if (warp == 9) {
       // ---- matrix products
       const uint32_t q_at = smem_addr(smem);
@@ -399,7 +469,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         if (sl >= L::kSlots) { sl -= L::kSlots; ph ^= 1u; }
       };
       auto scores = [&](int st, int sl) {                    // S = Q K^T
-        if (lane == 0) {
+        if (one()) {
           const uint64_t qd = operand(q_at + (kWide ? st * kTileBytes : 0), 16, 1024);
           const uint64_t kd = operand(smem_addr(smem + L::kRing + sl * kTileBytes), 16, 1024);
 #pragma unroll
@@ -410,7 +480,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         }
       };
       auto values = [&](int st, int sl, bool add) {          // O += P V
-        if (lane == 0) {
+        if (one()) {
           const uint64_t vd = operand(smem_addr(smem + L::kRing + sl * kTileBytes), kHalfBytes, 1024);
 #pragma unroll
           for (int k = 0; k < 8; ++k)
@@ -418,7 +488,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         }
       };
       auto commit = [&](uint64_t* bar) {
-        if (lane == 0) tc_commit(bar);
+        if (one()) tc_commit(bar);
       };
       // V rows behind the tile's last token may hold anything, and 0 * NaN must not reach the sums
       auto clear_tail = [&](const Seg& s, int t, int sl) {
@@ -430,6 +500,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
       };
+      lists([&] {
       for (int i = 0; ok && i < count; ++i) {
         const Seg s = list[i];
         if (rb * L::kRows >= s.nd * g) continue;
@@ -454,14 +525,12 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
             unsigned pv, pk;
             place(0, sv, pv);
             place(1, sk, pk);
+            if (!(ok = bar_wait(full + sv, pv, stop))) break;
+            clear_tail(s, s.t0 + t, sv);
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
               if (ok) ok = bar_wait(p_full + st, (p_phase >> st) & 1u, stop);
               p_phase ^= 1u << st;
-              if (ok && st == 0) {
-                ok = bar_wait(full + sv, pv, stop);
-                if (ok) clear_tail(s, s.t0 + t, sv);
-              }
               if (!ok) break;
               tc_fence_after();
               values(st, sv, t > 0);
@@ -486,12 +555,12 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
           }
           for (int t = 0; ok && t < n; ++t) {
             const int st = t & 1;
+            place(0, sl, ph);
+            if (!(ok = bar_wait(full + sl, ph, stop))) break;
+            clear_tail(s, s.t0 + t, sl);
             ok = bar_wait(p_full + st, (p_phase >> st) & 1u, stop);
             p_phase ^= 1u << st;
-            place(0, sl, ph);
-            if (ok) ok = bar_wait(full + sl, ph, stop);
             if (!ok) break;
-            clear_tail(s, s.t0 + t, sl);
             tc_fence_after();
             values(st, sl, t > 1);
             commit(empty + sl);
@@ -509,12 +578,18 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
           }
         }
       }
+      });
     } else {
+      lists([] {});
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
       // ---- softmax
       const int st = warp >> 2;
       const uint32_t lane_at = (uint32_t)((warp & 3) * 32) << 16;
       const uint32_t s_at = tmem + lane_at + st * kTile;
       const float scale = 0.08838834764831845f * kLog2e;     // 1 / sqrt(128), in the log2 domain
+      lists([&] {
       for (int i = 0; ok && i < count; ++i) {
         const Seg s = list[i];
         const int rows = min(L::kRows, s.nd * g - rb * L::kRows);   // valid rows of this block
@@ -543,17 +618,15 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
           const int t = s.t0 + (kWide ? k : 2 * k + st);
           // which of the tile's tokens the row sees
           uint32_t see[4] = {0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu};
-          bool partial = false;
-          if (busy) {
+          const bool partial = a.list != nullptr || t >= s.ctx_tiles || (t + 1) * kTile > s.ctx_tokens;
+          if (busy && partial) {
             const int at = t < s.ctx_tiles ? t * kTile : (t - s.ctx_tiles) * kTile;
             const int left = (t < s.ctx_tiles ? s.ctx_tokens : s.nd) - at;
             if (left < kTile) {
-              partial = true;
 #pragma unroll
               for (int w = 0; w < 4; ++w) see[w] = left >= 32 * w + 32 ? 0xFFFFFFFFu : left > 32 * w ? (1u << (left - 32 * w)) - 1u : 0u;
             }
             if (t >= s.ctx_tiles) {
-              partial = true;
               if (a.mask == nullptr) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -577,37 +650,28 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
                   see[w] &= w < n_pages && (((uint32_t)pages[w].y >> h_row) & 1u) ? 0xFFFFFFFFu : 0u;
                 }
               }
-              partial = true;
             }
           }
           if (!(ok = bar_wait(s_full + st, s_phase, stop))) break;
           s_phase ^= 1u;
           tc_fence_after();
           if (busy) {
-            // a half of the columns at a time (the registers hold one): the second half is looked over for its maximum,
-            // the first looked over and kept, the second read again when its turn comes
-            uint32_t x[2][32];
-            auto fetch = [&](int half) {
-              tmem_ld32(x[0], s_at + 64 * half);
-              tmem_ld32(x[1], s_at + 64 * half + 32);
-              tmem_wait_ld();
-              if (partial) {
+            uint32_t x[4][32];
 #pragma unroll
-                for (int w = 0; w < 2; ++w)
+            for (int w = 0; w < 4; ++w) tmem_ld32(x[w], s_at + 32 * w);
+            tmem_wait_ld();
+            if (partial) {
 #pragma unroll
-                  for (int e = 0; e < 32; ++e)
-                    if (!((see[2 * half + w] >> e) & 1u)) x[w][e] = 0xFF800000u;   // -inf, whatever the padding held
-              }
-            };
+              for (int w = 0; w < 4; ++w)
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                  if (!((see[w] >> e) & 1u)) x[w][e] = 0xFF800000u;   // -inf, whatever the padding held
+            }
             float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int half = 1; half >= 0; --half) {
-              fetch(half);
+            for (int w = 0; w < 4; ++w)
 #pragma unroll
-              for (int w = 0; w < 2; ++w)
-#pragma unroll
-                for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(x[w][e]));
-            }
+              for (int e = 0; e < 32; e += 2) mx[w] = max3(mx[w], __uint_as_float(x[w][e]), __uint_as_float(x[w][e + 1]));
             const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
             if (k == 0) {
               m = top;
@@ -619,36 +683,48 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
                 l *= factor;
                 const uint32_t o_at = tmem + lane_at + 256 + st * kTile;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                  uint32_t o[32];
-                  tmem_ld32(o, o_at + 32 * w);
+                for (int w = 0; w < 8; ++w) {
+                  uint32_t o[16];
+                  tmem_ld16(o, o_at + 16 * w);
                   tmem_wait_ld();
 #pragma unroll
-                  for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-                  tmem_st32(o_at + 32 * w, o);
+                  for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                  tmem_st16(o_at + 16 * w, o);
                 }
                 tmem_wait_st();
               }
             }
             const float ref = m == -INFINITY ? 0.f : -m;
-            // P is rounded to bf16 for the matrix product with V (half a step, 2^-9 of each weight); the sum keeps fp32
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            // P is rounded to bf16 for the matrix product with V (half a step, 2^-8 of each weight at most); the sum keeps fp32
+            pair_t sum[2] = {0ull, 0ull};
+            const pair_t scale2 = pair_of(scale, scale), ref2 = pair_of(ref, ref);
+            auto weigh = [&](auto mixed) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              if (half == 1) fetch(1);
-              uint32_t p[32];
+              for (int w = 0; w < 4; ++w) {
+                uint32_t p[16];
 #pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                const float p0 = exp2_fast(fmaf(__uint_as_float(x[e >> 4][(2 * e) & 31]), scale, ref));
-                const float p1 = exp2_fast(fmaf(__uint_as_float(x[e >> 4][(2 * e + 1) & 31]), scale, ref));
-                sum[e & 1] += p0;
-                sum[2 + (e & 1)] += p1;
-                const __nv_bfloat162 pair = __floats2bfloat162_rn(p0, p1);
-                p[e] = *reinterpret_cast<const uint32_t*>(&pair);
+                for (int e = 0; e < 16; ++e) {
+                  pair_t y = fma2(pair_of(__uint_as_float(x[w][2 * e]), __uint_as_float(x[w][2 * e + 1])), scale2, ref2);
+                  float p0, p1;
+                  if (decltype(mixed)::value && kByFma >> (e & 7) & 1) {
+                    exp2_pair(y, p0, p1);
+                  } else {
+                    unpair(y, p0, p1);
+                    p0 = exp2_fast(p0);
+                    p1 = exp2_fast(p1);
+                  }
+                  sum[e & 1] = add2(sum[e & 1], pair_of(p0, p1));
+                  const __nv_bfloat162 pair = __floats2bfloat162_rn(p0, p1);
+                  p[e] = *reinterpret_cast<const uint32_t*>(&pair);
+                }
+                tmem_st16(s_at + 16 * w, p);
               }
-              tmem_st32(s_at + 32 * half, p);
-            }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            };
+            if (partial) weigh(std::false_type());           // (-inf has to give 0)
+            else weigh(std::true_type());
+            float s0, s1;
+            unpair(add2(sum[0], sum[1]), s0, s1);
+            l += s0 + s1;
             tmem_wait_st();
           }
           tc_fence_before();
@@ -741,11 +817,9 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
           j_phase ^= 1u;
         }
       }
-    }
-    first_list = false;
-    __syncthreads();
-    if (*stop != 0) break;
+      });
   }
+  __syncthreads();
 
   if (*stop != 0) {
     // a wait ran out: copies and products under way still write to this CTA's memory
@@ -757,7 +831,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
       }
     }
     if (warp == 9) {
-      if (lane == 0) tc_commit(drained);
+      if (one()) tc_commit(drained);
       for (unsigned polls = 0; polls < kWaitLimit && !bar_try(drained, 0u); ++polls) { }
     }
   }
