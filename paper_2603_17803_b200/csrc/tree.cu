@@ -192,7 +192,7 @@ __device__ __forceinline__ pair_t add2(pair_t a, pair_t b) {
 // relative error, 2.1e-7 in fp32), n added to the exponent.  It runs on the multiply-add units, beside the exponentials of the
 // special function unit (kByFma: which pairs of eight), which a tile of 256 rows would keep busy for longer than its K and V
 // take to arrive.
-constexpr unsigned kByFma = 0x52u;
+constexpr unsigned kByFma = 0x11u;
 __device__ __forceinline__ void exp2_pair(pair_t y, float& lo, float& hi) {
   float y0, y1;
   unpair(y, y0, y1);
