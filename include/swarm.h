@@ -474,8 +474,8 @@ int32_t swarm_build_clusters(const float* dist, int32_t n_entries, float tau, vo
  * were; n_draft outside 0..T sets it too and is clamped.
  * Reads inputs->kv_pool, page_base, ctx_len.  workspace: swarm_tree_attn_workspace_bytes(shape, T) bytes of device
  * memory (256-byte aligned, contents irrelevant), used by one call at a time; < 0: minus an error code.
- * SWARM_ERR_UNSUPPORTED: n_pool_pages >= 2^31; with a selection, more than 32 query heads per KV head or more than 655360
- * pages per request. */
+ * SWARM_ERR_UNSUPPORTED: n_pool_pages >= 2^31 or more than 128 query heads per KV head; with a selection, more than 32 query
+ * heads per KV head or more than 655360 pages per request. */
 int64_t swarm_tree_attn_workspace_bytes(const swarm_shape* shape, int32_t max_draft);
 int32_t swarm_tree_attn(swarm_ctx* ctx, const swarm_inputs* inputs, const swarm_tree* tree, const int32_t* sel,
                         const int32_t* n_sel, void* workspace, int64_t workspace_bytes, void* out, float* lse, void* stream);

@@ -6,13 +6,15 @@
 // The g query heads of a KV head and the drafted tokens of a request see the same keys: they are the up to 256 rows of one
 // matrix product with every tile of 128 tokens, so K and V are read once for all of them.
 //
-//   warps 0-3, 4-7   two softmax streams, a thread per row of 128 (tcgen05.ld: lane = row)
+//   warps 0-3, 4-7   two softmax streams, a thread per row of 128 (tcgen05.ld: lane = row), which holds the 128 scores of a tile in
+//                    registers (setmaxnreg: two threads per row, with 64 each, gained nothing and spilled)
 //   warp 8           copies: K and V tiles of 32 KB by TMA into a ring, 128-byte swizzle
-//   warp 11          lists the CTA's share of the work (warp 10 only fills the warpgroup, whose registers go to the softmax)
 //   warp 9           matrix products: S = Q K^T (operands in shared memory), O += P V (P from tensor memory)
+//   warp 10          copies of the units' queries, each as soon as the last product with the one before is done
+//   warp 11          lists the CTA's share of the work
 // Tensor memory: S0, S1 (128 columns each; P, in bf16, takes the place of S), O0, O1.  While one stream is in its softmax
 // the tensor core works for the other.  Up to 128 rows: the streams take alternate tiles of the same rows, and their
-// sums are joined at the end through tensor memory; beyond, each has 128 rows of its own and both use every tile.
+// sums are joined at the end through tensor memory; beyond (kWide), each has 128 rows of its own and both use every tile.
 //
 // The tiles of all (request, KV head) units form one list that is cut evenly over the CTAs, whatever the lengths
 // are; a unit that is cut leaves partial (m, l, O) per CTA, joined by a second kernel with a warp per row.
@@ -30,7 +32,10 @@ namespace {
 constexpr int kTile = 128;                                 // tokens of a tile, rows of a stream
 constexpr int kTileBytes = kTile * kHeadDim * 2;           // K or V of a tile: two halves of 64 coordinates
 constexpr int kHalfBytes = kTileBytes / 2;
-constexpr int kThreads = 384;
+constexpr int kSoftWarps = 8;
+constexpr int kThreads = (kSoftWarps + 4) * 32;
+constexpr int kLoadWarp = kSoftWarps, kMmaWarp = kSoftWarps + 1, kQueryWarp = kSoftWarps + 2,
+              kListWarp = kSoftWarps + 3;
 constexpr int kSegs = 32;                                  // segments of a CTA listed at a time
 constexpr int kMaxTreeCtas = 148;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -59,7 +64,7 @@ struct Layout {
   static constexpr int kRing = kQTiles * kTileBytes;
   static constexpr int kBars = kRing + kSlots * kTileBytes;
   static constexpr int kList = kBars + 256;
-  static constexpr int kMl = kList + kSegs * (int)sizeof(Seg);
+  static constexpr int kMl = kList + kSegs * (int)sizeof(Seg);   // (m, l) of [stream][row]
   static constexpr int kScan = kMl + 2 * kTile * 8;
   static constexpr int kBytes = kScan + 256;
 };
@@ -96,10 +101,10 @@ __device__ __forceinline__ bool bar_wait(uint64_t* bar, unsigned parity, volatil
   if (!there) *stop = 1;
   return __all_sync(0xFFFFFFFFu, there);
 }
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int c1, int c2, int c3, int c4, uint64_t* bar) {
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, int c4, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
-      "l"(map), "r"(0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(smem_addr(bar))
+      "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(smem_addr(bar))
       : "memory");
 }
 
@@ -228,7 +233,8 @@ struct TreeArgs {
   const int32_t* list_tokens; // [B*Hkv] context tokens among them
   int list_cap;
   int T, words, row_blocks, chunks;
-  float* part_o;              // [CTA][2][rows][128]
+  int tile_tokens;            // drafted tokens of a tile of rows: row r of a tile is token r / g of it, head r % g
+  float4* part_o;             // [CTA][2][32 groups of four coordinates][rows]
   float2* part_ml;            // [CTA][2][rows]
   int32_t* unit_first;        // [B*Hkv] 2 * chunk + place of the unit's first partial
   int32_t* unit_last;         // [B*Hkv] its last chunk
@@ -259,35 +265,39 @@ __device__ __forceinline__ int tiles_of(int ctx, int nd) {
 template <bool kWide>
 __global__ void __launch_bounds__(kThreads, 1)
 tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_constant__ CUtensorMap pool_page,
-                 const __grid_constant__ CUtensorMap draft_k, const __grid_constant__ CUtensorMap draft_v, const TreeArgs a) {
+                 const __grid_constant__ CUtensorMap draft_k, const __grid_constant__ CUtensorMap draft_v,
+                 const __grid_constant__ CUtensorMap queries, const TreeArgs a) {
   using L = Layout<kWide>;
   extern __shared__ __align__(1024) unsigned char smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBars);
   uint64_t *full = bars, *empty = bars + 6, *s_full = bars + 12, *p_full = bars + 14, *q_full = bars + 16, *joined = bars + 17,
-           *drained = bars + 18;
-  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + 20);
-  volatile int* stop = reinterpret_cast<volatile int*>(bars + 21);
-  int* n_segs = reinterpret_cast<int*>(bars + 22);
+           *drained = bars + 18, *q_empty = bars + 19, *o_full = bars + 20;
+  uint32_t* tmem_at = reinterpret_cast<uint32_t*>(bars + 22);
+  volatile int* stop = reinterpret_cast<volatile int*>(bars + 23);
+  int* n_segs = reinterpret_cast<int*>(bars + 24);
   Seg* list = reinterpret_cast<Seg*>(smem + L::kList);
-  float2* ml = reinterpret_cast<float2*>(smem + L::kMl);     // [2][128] of the two streams
-  long long* scan = reinterpret_cast<long long*>(smem + L::kScan);
+  float2* ml = reinterpret_cast<float2*>(smem + L::kMl);
+  int* scan = reinterpret_cast<int*>(smem + L::kScan);
 
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);    // (known to be the same for the whole warp: see `one`)
   const int rb = blockIdx.x % a.row_blocks, chunk = blockIdx.x / a.row_blocks;
   const int g = a.geo.g, Hkv = a.geo.Hkv, S = a.geo.S;
   const int units = a.geo.B * Hkv;
+  const int first_tile = rb * L::kQTiles;                    // of rows
+  const auto row_tiles = [&](int nd) { return (nd + a.tile_tokens - 1) / a.tile_tokens - first_tile; };   // <= 0: none for this CTA
 
   if (tid == 0) {
     for (int i = 0; i < L::kSlots; ++i) { bar_init(full + i, 1); bar_init(empty + i, 1); }
-    for (int i = 0; i < 2; ++i) { bar_init(s_full + i, 1); bar_init(p_full + i, 4); }
-    bar_init(q_full, 8);
-    bar_init(joined, 8);
+    for (int i = 0; i < 2; ++i) { bar_init(s_full + i, 1); bar_init(o_full + i, 1); bar_init(p_full + i, kSoftWarps / 2); }
+    bar_init(q_full, 1);
+    bar_init(q_empty, 1);
+    bar_init(joined, kSoftWarps);
     bar_init(drained, 1);
     *stop = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 9) {
+  if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(tmem_at)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     tc_fence_before();
@@ -295,37 +305,43 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
   pdl_wait();
   pdl_launch_dependents();
 
-  // ---- this CTA's share of all tiles: the list of units is summed by the whole CTA, the unit of its first tile found
+  // ---- this CTA's share of all tiles: the list of units is summed by the whole CTA, the unit of its first tile found.  Up to a
+  // unit per thread, their lengths stay in shared memory (the ring is still empty) for the first list of segments.
+  int2* lengths = reinterpret_cast<int2*>(smem + L::kRing);
+  const bool cached = units <= kThreads;
   const int per = (units + kThreads - 1) / kThreads;
   const int u_lo = min(units, tid * per), u_hi = min(units, u_lo + per);
-  long long mine = 0;
+  int mine = 0;
   for (int u = u_lo; u < u_hi; ++u) {
     int ctx, nd;
     bool bad;
     unit_lengths(a, u, ctx, nd, bad);
     if (bad && blockIdx.x == 0 && u % Hkv == 0) atomicOr(a.status, SWARM_DEV_BAD_LENGTH);
+    if (cached) lengths[u] = make_int2(ctx, nd);
     mine += tiles_of(ctx, nd);
   }
-  long long incl = mine;
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (in front of the copies that go there)
+  int incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+    const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
     if (lane >= o) incl += v;
   }
   if (lane == 31) scan[warp] = incl;
   __syncthreads();
   tc_fence_after();
-  long long before = incl - mine, total = 0;
+  int before = incl - mine, total = 0;
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) {
-    if (w < warp) before += scan[w];
-    total += scan[w];
+    const int v = scan[w];
+    if (w < warp) before += v;
+    total += v;
   }
-  const long long w0 = total * chunk / a.chunks, w1 = total * (chunk + 1) / a.chunks;
+  const int each = total / a.chunks, more = total - each * a.chunks;   // the first `more` CTAs take one tile more
+  const int w0 = chunk * each + min(chunk, more), w1 = w0 + each + (chunk < more ? 1 : 0);
   if (w0 < w1 && before <= w0 && w0 < before + mine) {       // one thread: its units hold the first tile
-    int u = u_lo;
-    long long at = before;
-    for (; u < u_hi; ++u) {
+    int u = u_lo, at = before;
+    for (; u + 1 < u_hi; ++u) {
       int ctx, nd;
       bool bad;
       unit_lengths(a, u, ctx, nd, bad);
@@ -343,11 +359,11 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
   int slot = 0;
   unsigned ring_phase = 0u;                                  // parity of the current round through the ring
   unsigned s_phase = 0u, p_phase = 0u, q_phase = 0u, j_phase = 0u;   // (p_phase: a bit per stream)
-  int issued = 0;                                            // copies started (producer)
+  int issued = 0, asked = 0;                                 // copies started of tiles, of queries
   bool ok = true;
   bool first_list = true;
-  int u_next = w0 < w1 ? (int)scan[kThreads / 32] : units;
-  long long at_next = w0 < w1 ? scan[kThreads / 32 + 1] : 0;
+  int u_next = w0 < w1 ? scan[kThreads / 32] : units;
+  int at_next = w0 < w1 ? scan[kThreads / 32 + 1] : 0;
 
   int count = 0;
   // Calls `work` for one list of segments after the other; every warp of the CTA goes through the same lists.
@@ -355,30 +371,36 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
     while (u_next < units && at_next < w1) {
       __syncthreads();                                       // the previous list has been worked through
       if (*stop != 0) break;
-      if (warp == 11) {                                      // the next (up to 32) units with tiles in this CTA's share
+      if (warp == kListWarp) {                                   // the next (up to 32) units with tiles in this CTA's share
         const int u = u_next + lane;
         int ctx = 0, nd = 0, n = 0;
         bool bad;
         if (u < units) {
-          unit_lengths(a, u, ctx, nd, bad);
+          if (cached && first_list) {
+            const int2 v = lengths[u];
+            ctx = v.x;
+            nd = v.y;
+          } else {
+            unit_lengths(a, u, ctx, nd, bad);
+          }
           n = tiles_of(ctx, nd);
         }
-        long long end = n;
+        int end = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-          const long long v = __shfl_up_sync(0xFFFFFFFFu, end, o);
+          const int v = __shfl_up_sync(0xFFFFFFFFu, end, o);
           if (lane >= o) end += v;
         }
         end += at_next;
-        const long long begin = end - n;
+        const int begin = end - n;
         const bool here = n > 0 && begin < w1 && end > w0;
         const unsigned all = __ballot_sync(0xFFFFFFFFu, here);
         if (here) {
           Seg s;
           s.b = u / Hkv;
           s.kv = u - s.b * Hkv;
-          s.t0 = (int)(max(w0, begin) - begin);
-          s.t1 = (int)(min(w1, end) - begin);
+          s.t0 = max(w0, begin) - begin;
+          s.t1 = min(w1, end) - begin;
           s.ctx_tiles = (ctx + kTile - 1) / kTile;
           s.ctx_tokens = ctx;
           s.nd = nd;
@@ -401,9 +423,9 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
     }
   };
 
-  if (warp >= 8) {
+  if (warp >= kSoftWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");     // 128 * 72 + 256 * 216 = 384 * 168, what the CTA was launched with
-    if (warp == 8) {
+    if (warp == kLoadWarp) {
       // ---- copies, in the order the matrix products use them
       auto load_tile = [&](const Seg& s, int t, int which) -> bool {   // which: 0 = K, 1 = V
         if (issued >= L::kSlots && !bar_wait(empty + slot, ring_phase ^ 1u, stop)) return false;
@@ -412,12 +434,12 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         if (t >= s.ctx_tiles) {                              // drafted tokens; rows behind the last are filled with zeros
           if (lane == 0) {
             bar_expect(bar, kTileBytes);
-            tma_load(dst, which == 0 ? &draft_k : &draft_v, (t - s.ctx_tiles) * kTile, 0, s.kv, s.b, bar);
+            tma_load(dst, which == 0 ? &draft_k : &draft_v, 0, (t - s.ctx_tiles) * kTile, 0, s.kv, s.b, bar);
           }
         } else if (a.list == nullptr) {
           if (lane == 0) {
             bar_expect(bar, kTileBytes);
-            tma_load(dst, &pool_tile, 0, (int)(a.page_base[s.b] + (long long)t * (kTile / S)), 0, s.kv * 2 + which, bar);
+            tma_load(dst, &pool_tile, 0, 0, (int)(a.page_base[s.b] + (long long)t * (kTile / S)), 0, s.kv * 2 + which, bar);
           }
         } else {                                             // the tile's pages one by one, a lane each
           const int per_tile = kTile / S, pages = min(per_tile, (s.ctx_tokens + S - 1) / S - t * per_tile);
@@ -426,7 +448,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
           if (lane < pages) {
             const int page = (int)a.page_base[s.b] + a.list[(long long)(s.b * Hkv + s.kv) * a.list_cap + t * per_tile + lane].x;
             for (int h = 0; h < 2; ++h)
-              tma_load(dst + h * kHalfBytes + lane * S * 128, &pool_page, 0, page, h, s.kv * 2 + which, bar);
+              tma_load(dst + h * kHalfBytes + lane * S * 128, &pool_page, 0, 0, page, h, s.kv * 2 + which, bar);
           }
         }
         __syncwarp();
@@ -437,9 +459,9 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
       lists([&] {
       for (int i = 0; ok && i < count; ++i) {
         const Seg s = list[i];
-        if (rb * L::kRows >= s.nd * g) continue;
+        if (row_tiles(s.nd) <= 0) continue;
         const int n = s.t1 - s.t0;
-        if constexpr (kWide) {
+        if (kWide && row_tiles(s.nd) > 1) {
           ok = load_tile(s, s.t0, 0);
           for (int t = 0; ok && t < n; ++t) {
             ok = load_tile(s, s.t0 + t, 1);
@@ -455,7 +477,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         }
       }
       });
-    } else if (warp == 9) {
+    } else if (warp == kMmaWarp) {
       // ---- matrix products
       const uint32_t q_at = smem_addr(smem);
       auto advance = [&](int n) {
@@ -468,9 +490,9 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         ph = ring_phase;
         if (sl >= L::kSlots) { sl -= L::kSlots; ph ^= 1u; }
       };
-      auto scores = [&](int st, int sl) {                    // S = Q K^T
+      auto scores = [&](int st, int sl, int q_tile) {        // S = Q K^T
         if (one()) {
-          const uint64_t qd = operand(q_at + (kWide ? st * kTileBytes : 0), 16, 1024);
+          const uint64_t qd = operand(q_at + q_tile * kTileBytes, 16, 1024);
           const uint64_t kd = operand(smem_addr(smem + L::kRing + sl * kTileBytes), 16, 1024);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
@@ -503,7 +525,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
       lists([&] {
       for (int i = 0; ok && i < count; ++i) {
         const Seg s = list[i];
-        if (rb * L::kRows >= s.nd * g) continue;
+        if (row_tiles(s.nd) <= 0) continue;
+        const bool wide = kWide && row_tiles(s.nd) > 1;
         const int n = s.t1 - s.t0;
         ok = bar_wait(q_full, q_phase, stop);
         q_phase ^= 1u;
@@ -511,14 +534,15 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         tc_fence_after();
         int sl;
         unsigned ph;
-        if constexpr (kWide) {
+        if (wide) {
           place(0, sl, ph);
           if (!(ok = bar_wait(full + sl, ph, stop))) break;
-          scores(0, sl);
+          scores(0, sl, 0);
           commit(s_full);
-          scores(1, sl);
+          scores(1, sl, 1);
           commit(s_full + 1);
           commit(empty + sl);
+          if (n == 1) commit(q_empty);
           advance(1);
           for (int t = 0; ok && t < n; ++t) {
             int sv, sk;
@@ -537,10 +561,11 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
               if (st == 1) commit(empty + sv);
               if (t + 1 < n) {
                 if (st == 0 && !(ok = bar_wait(full + sk, pk, stop))) break;
-                scores(st, sk);
+                scores(st, sk, st);
                 if (st == 1) commit(empty + sk);
+                if (st == 1 && t + 2 == n) commit(q_empty);
               }
-              commit(s_full + st);
+              commit(t + 1 < n ? s_full + st : o_full + st);
             }
             advance(t + 1 < n ? 2 : 1);
           }
@@ -548,11 +573,12 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
           for (int st = 0; ok && st < min(n, 2); ++st) {
             place(0, sl, ph);
             if (!(ok = bar_wait(full + sl, ph, stop))) break;
-            scores(st, sl);
+            scores(st, sl, 0);
             commit(s_full + st);
             commit(empty + sl);
             advance(1);
           }
+          if (ok && n <= 2) commit(q_empty);
           for (int t = 0; ok && t < n; ++t) {
             const int st = t & 1;
             place(0, sl, ph);
@@ -568,78 +594,80 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
             if (t + 2 < n) {
               place(0, sl, ph);
               if (!(ok = bar_wait(full + sl, ph, stop))) break;
-              scores(st, sl);
+              scores(st, sl, 0);
               commit(s_full + st);
               commit(empty + sl);
+              if (t + 3 == n) commit(q_empty);
               advance(1);
             } else {
-              commit(s_full + st);
+              commit(o_full + st);
             }
           }
         }
       }
+      });
+    } else if (warp == kQueryWarp) {
+      lists([&] {
+        for (int i = 0; ok && i < count; ++i) {
+          const Seg s = list[i];
+          if (row_tiles(s.nd) <= 0) continue;
+          if (asked > 0 && !(ok = bar_wait(q_empty, q_phase, stop))) break;
+          if (asked > 0) q_phase ^= 1u;
+          const int tiles = min(L::kQTiles, row_tiles(s.nd));
+          if (lane == 0) {
+            bar_expect(q_full, (unsigned)(tiles * a.tile_tokens * g * kHeadDim * 2));
+            for (int j = 0; j < 2 * tiles; ++j)              // a tile's halves of 64 coordinates; tokens behind the last are zeros
+              tma_load(smem_addr(smem + (j >> 1) * kTileBytes + (j & 1) * kHalfBytes), &queries, (j & 1) * 64, 0,
+                       (first_tile + (j >> 1)) * a.tile_tokens, s.kv, s.b, q_full);
+          }
+          __syncwarp();
+          ++asked;
+        }
       });
     } else {
       lists([] {});
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-      // ---- softmax
-      const int st = warp >> 2;
-      const uint32_t lane_at = (uint32_t)((warp & 3) * 32) << 16;
-      const uint32_t s_at = tmem + lane_at + st * kTile;
-      const float scale = 0.08838834764831845f * kLog2e;     // 1 / sqrt(128), in the log2 domain
-      lists([&] {
+    // ---- softmax
+    const int st = warp >> 2, lane_row = (warp & 3) * 32 + lane;
+    const uint32_t lane_at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t s_at = lane_at + st * kTile, o_at = lane_at + 256 + st * kTile;
+    unsigned o_phase = 0u;
+    const float scale = 0.08838834764831845f * kLog2e;       // 1 / sqrt(128), in the log2 domain
+    lists([&] {
       for (int i = 0; ok && i < count; ++i) {
         const Seg s = list[i];
-        const int rows = min(L::kRows, s.nd * g - rb * L::kRows);   // valid rows of this block
-        if (rows <= 0) continue;
-        // the unit's queries, swizzled like the tiles; rows that do not exist are zeros
-        for (int c = tid; c < L::kRows * 16; c += 256) {
-          const int r = c >> 4, ch = c & 15, row = rb * L::kRows + r, t = row / g;
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (r < rows)
-            v = ldg_nc_v4(a.q + (((long long)s.b * a.T + t) * a.geo.Hq + s.kv * g + (row - t * g)) * kHeadDim + ch * 8);
-          *reinterpret_cast<uint4*>(smem + (r >> 7) * kTileBytes + (ch >> 3) * kHalfBytes + (r & 127) * 128 +
-                                    (((ch & 7) ^ (r & 7)) << 4)) = v;
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) bar_arrive(q_full);
-
-        const int r = (kWide ? st * kTile : 0) + (warp & 3) * 32 + lane;   // this thread's row of the block
-        const int row = rb * L::kRows + r, t_row = row / g, h_row = row - t_row * g;
-        const bool busy = r - lane < rows;                   // some row of the warp exists
+        if (row_tiles(s.nd) <= 0) continue;
+        const bool wide = kWide && row_tiles(s.nd) > 1;
+        const int tile_first = (first_tile + (wide ? st : 0)) * a.tile_tokens;   // first token of this stream's rows
+        const int t_row = tile_first + lane_row / g, h_row = lane_row % g;       // this thread's row
+        const int rows = min(a.tile_tokens, s.nd - tile_first) * g;              // of the stream
+        const bool there = lane_row < rows, busy = lane_row - lane < rows;       // busy: some row of the warp exists
         const int n = s.t1 - s.t0;
-        const int my_n = kWide ? n : (n + 1 - st) >> 1;
+        const int my_n = wide ? n : (n + 1 - st) >> 1;
         float m = -INFINITY, l = 0.f;
         for (int k = 0; k < my_n; ++k) {
-          const int t = s.t0 + (kWide ? k : 2 * k + st);
+          const int t = s.t0 + (wide ? k : 2 * k + st);
           // which of the tile's tokens the row sees
           uint32_t see[4] = {0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu};
           const bool partial = a.list != nullptr || t >= s.ctx_tiles || (t + 1) * kTile > s.ctx_tokens;
           if (busy && partial) {
-            const int at = t < s.ctx_tiles ? t * kTile : (t - s.ctx_tiles) * kTile;
-            const int left = (t < s.ctx_tiles ? s.ctx_tokens : s.nd) - at;
-            if (left < kTile) {
+            const int first = (t < s.ctx_tiles ? t : t - s.ctx_tiles) * kTile;   // of the context or of the drafted tokens
+            const int left = (t < s.ctx_tiles ? s.ctx_tokens : s.nd) - first;
 #pragma unroll
-              for (int w = 0; w < 4; ++w) see[w] = left >= 32 * w + 32 ? 0xFFFFFFFFu : left > 32 * w ? (1u << (left - 32 * w)) - 1u : 0u;
-            }
+            for (int w = 0; w < 4; ++w) see[w] = left >= 32 * w + 32 ? 0xFFFFFFFFu : left > 32 * w ? (1u << (left - 32 * w)) - 1u : 0u;
             if (t >= s.ctx_tiles) {
-              if (a.mask == nullptr) {
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                  const int first = at + 32 * w;
-                  see[w] &= t_row >= first + 31 ? 0xFFFFFFFFu : t_row >= first ? (2u << (t_row - first)) - 1u : 0u;
-                }
-              } else if (t_row < s.nd) {
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                  see[w] &= at / 32 + w < a.words ? a.mask[((long long)s.b * a.T + t_row) * a.words + at / 32 + w] : 0u;
+              for (int w = 0; w < 4; ++w) {
+                const int at = first + 32 * w;
+                if (a.mask == nullptr)
+                  see[w] &= t_row >= at + 31 ? 0xFFFFFFFFu : t_row >= at ? (2u << (t_row - at)) - 1u : 0u;
+                else if (t_row < s.nd)
+                  see[w] &= at / 32 < a.words ? a.mask[((long long)s.b * a.T + t_row) * a.words + at / 32] : 0u;
               }
             } else if (a.list != nullptr) {
-              const int2* pages = a.list + (long long)(s.b * Hkv + s.kv) * a.list_cap + t * (kTile / S);
+              const int2* pages = a.list + (long long)(s.b * Hkv + s.kv) * a.list_cap + first / S;
               const int n_pages = (left + S - 1) / S;
 #pragma unroll
               for (int w = 0; w < 4; ++w) {
@@ -681,7 +709,6 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
                 const float factor = raise ? exp2_fast(m - top) : 1.f;
                 if (raise) m = top;
                 l *= factor;
-                const uint32_t o_at = tmem + lane_at + 256 + st * kTile;
 #pragma unroll
                 for (int w = 0; w < 8; ++w) {
                   uint32_t o[16];
@@ -704,7 +731,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
                 uint32_t p[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                  pair_t y = fma2(pair_of(__uint_as_float(x[w][2 * e]), __uint_as_float(x[w][2 * e + 1])), scale2, ref2);
+                  const pair_t y = fma2(pair_of(__uint_as_float(x[w][2 * e]), __uint_as_float(x[w][2 * e + 1])), scale2, ref2);
                   float p0, p1;
                   if (decltype(mixed)::value && kByFma >> (e & 7) & 1) {
                     exp2_pair(y, p0, p1);
@@ -733,54 +760,51 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         }
         if (!ok) break;
         if (my_n > 0) {
-          if (!(ok = bar_wait(s_full + st, s_phase, stop))) break;   // the last product with V is complete
-          s_phase ^= 1u;
+          if (!(ok = bar_wait(o_full + st, o_phase, stop))) break;   // the last product with V is complete
+          o_phase ^= 1u;
         }
-        // up to 128 rows: both streams hold sums of the same rows; each warp joins 64 of the coordinates
+        // up to 128 rows both streams hold sums of the same rows; each thread joins half of the coordinates
         float a_own = 1.f, a_other = 0.f;
-        if constexpr (!kWide) {
-          ml[st * kTile + (warp & 3) * 32 + lane] = make_float2(m, l);
+        if (!wide) {
+          ml[st * kTile + lane_row] = make_float2(m, l);
           tc_fence_before();
           __syncwarp();
           if (lane == 0) bar_arrive(joined);
           if (!(ok = bar_wait(joined, j_phase, stop))) break;
           j_phase ^= 1u;
-          const float2 o = ml[(st ^ 1) * kTile + (warp & 3) * 32 + lane];
-          const float both = fmaxf(m, o.x);
+          tc_fence_after();
+          const float2 other = ml[(st ^ 1) * kTile + lane_row];
+          const float both = fmaxf(m, other.x);
           a_own = m == -INFINITY ? 0.f : exp2_fast(m - both);
-          a_other = o.x == -INFINITY ? 0.f : exp2_fast(o.x - both);
-          l = l * a_own + o.y * a_other;
+          a_other = other.x == -INFINITY ? 0.f : exp2_fast(other.x - both);
+          l = l * a_own + other.y * a_other;
           m = both;
+        } else {
+          tc_fence_after();
         }
-        tc_fence_after();
         if (busy) {
           const bool whole = s.t0 == 0 && s.last;
           const float inv = l > 0.f ? 1.f / l : 0.f;
-          const long long part = (long long)(blockIdx.x * 2 + (i == 0 && first_list ? 0 : 1)) * L::kRows + r;
+          const long long part = blockIdx.x * 2 + (i == 0 && first_list ? 0 : 1);
+          const int r = (wide ? st * kTile : 0) + lane_row;  // row of the block
           const long long at = ((long long)s.b * a.T + t_row) * a.geo.Hq + s.kv * g + h_row;
-          const bool other_on = !kWide && n > 1;             // (a stream without a tile has written no O)
-          const bool own_on = kWide || my_n > 0;
-#pragma unroll
-          for (int w = 0; w < (kWide ? 4 : 2); ++w) {
-            const int col = kWide ? 32 * w : 64 * st + 32 * w;
-            uint32_t o[32], o2[32];
-            tmem_ld32(o, tmem + lane_at + 256 + st * kTile + col);
-            if constexpr (!kWide) tmem_ld32(o2, tmem + lane_at + 256 + (st ^ 1) * kTile + col);
+          const bool own_on = my_n > 0, other_on = !wide && (st == 1 || n > 1);   // (a stream without a tile has written no O)
+          const int width = wide ? 128 : 64, col0 = wide ? 0 : st * 64;
+          for (int col = col0; col < col0 + width; col += 16) {
+            uint32_t o[16], o2[16];
+            tmem_ld16(o, lane_at + 256 + st * kTile + col);
+            if (!wide) tmem_ld16(o2, lane_at + 256 + (st ^ 1) * kTile + col);
             tmem_wait_ld();
-            float f[32];
+            float f[16];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              if constexpr (kWide) {
-                f[e] = __uint_as_float(o[e]);
-              } else {
-                f[e] = (own_on ? __uint_as_float(o[e]) * a_own : 0.f) +
-                       ((st == 0 ? other_on : true) ? __uint_as_float(o2[e]) * a_other : 0.f);
-              }
+            for (int e = 0; e < 16; ++e) {
+              f[e] = own_on ? __uint_as_float(o[e]) * a_own : 0.f;
+              if (other_on) f[e] += __uint_as_float(o2[e]) * a_other;
             }
-            if (r < rows) {
+            if (there) {
               if (whole) {
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
+                for (int e = 0; e < 16; e += 8) {
                   uint4 v;
                   uint32_t* pv = reinterpret_cast<uint32_t*>(&v);
 #pragma unroll
@@ -792,112 +816,161 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
                 }
               } else {
 #pragma unroll
-                for (int e = 0; e < 32; e += 4)
-                  __stcg(reinterpret_cast<float4*>(a.part_o + part * kHeadDim + col + e), make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]));
+                for (int e = 0; e < 16; e += 4)
+                  __stcg(a.part_o + (part * 32 + (col + e) / 4) * L::kRows + r, make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]));
               }
             }
           }
-          if (r < rows && (kWide || st == 0)) {
+          if (there && col0 == 0) {
             if (whole) a.lse[at] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
-            else __stcg(a.part_ml + part, make_float2(m, l));
+            else __stcg(a.part_ml + part * L::kRows + r, make_float2(m, l));
           }
         }
-        if constexpr (!kWide) {
-          // the other stream's warps read this stream's (m, l) and O: they have, once all have joined again
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) bar_arrive(joined);
-          if (!(ok = bar_wait(joined, j_phase, stop))) break;
-          j_phase ^= 1u;
-        } else {
-          // Q may be overwritten once both streams have seen their last scores
-          __syncwarp();
-          if (lane == 0) bar_arrive(joined);
-          if (!(ok = bar_wait(joined, j_phase, stop))) break;
-          j_phase ^= 1u;
-        }
+        // the rows' sums and O may be written again once all warps are here
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(joined);
+        if (!(ok = bar_wait(joined, j_phase, stop))) break;
+        j_phase ^= 1u;
       }
-      });
+    });
   }
   __syncthreads();
 
   if (*stop != 0) {
     // a wait ran out: copies and products under way still write to this CTA's memory
     if (tid == 0) atomicOr(a.status, SWARM_DEV_TIMEOUT);
-    if (warp == 8) {
+    if (warp == kLoadWarp) {
       for (int i = 0; i < min(issued, L::kSlots); ++i) {
         if (--slot < 0) { slot = L::kSlots - 1; ring_phase ^= 1u; }
         for (unsigned polls = 0; polls < kWaitLimit && !bar_try(full + slot, ring_phase); ++polls) { }
       }
     }
-    if (warp == 9) {
+    if (warp == kQueryWarp && asked > 0)
+      for (unsigned polls = 0; polls < kWaitLimit && !bar_try(q_full, (unsigned)(asked - 1) & 1u); ++polls) { }
+    if (warp == kMmaWarp) {
       if (one()) tc_commit(drained);
       for (unsigned polls = 0; polls < kWaitLimit && !bar_try(drained, 0u); ++polls) { }
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kMmaWarp) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
   }
 }
 
-// Joins the partial sums of the units that were cut: a warp per row, four coordinates per lane.
-template <int kRows>
+// Joins the partial sums of the units that were cut: a lane per row, 16 coordinates per warp, and kSplit warps that share a unit's
+// partials (few units are cut into many).  The partials lie with the rows innermost, so that both kernels touch whole lines.
+template <int kQTiles, int kSplit>
 __global__ void __launch_bounds__(256)
-tree_merge_kernel(const TreeArgs a) {
+tree_merge_kernel(const TreeArgs a, int groups, int tiles) {
+  constexpr int kRows = kQTiles * kTile, kCols = 8 / kSplit;  // kCols groups of 16 coordinates per CTA
+  __shared__ float s_ml[kSplit > 1 ? kSplit * 64 : 1];
+  __shared__ float s_o[kSplit > 1 ? kSplit * 16 * 32 : 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, split = warp / kCols;
+  int id = blockIdx.x;
+  const int col = (id % kSplit) * kCols + warp % kCols;
+  id /= kSplit;
+  const int group = id % groups;
+  id /= groups;
+  const int tile = id % tiles, u = id / tiles;
+  const int b = u / a.geo.Hkv, kv = u - b * a.geo.Hkv, g = a.geo.g;
+  const int in_tile = group * 32 + lane, t = tile * a.tile_tokens + in_tile / g, h = in_tile % g;
   pdl_wait();
-  pdl_launch_dependents();
-  const int lane = threadIdx.x & 31;
-  const long long at = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);   // [B][T][Hq]
-  if (at >= (long long)a.geo.B * a.T * a.geo.Hq) return;
-  const int h = (int)(at % a.geo.Hq), t = (int)(at / a.geo.Hq % a.T), b = (int)(at / a.geo.Hq / a.T);
-  const int kv = h / a.geo.g, u = b * a.geo.Hkv + kv;
+  const int first = a.unit_first[u], last = a.unit_last[u];  // (not written where nd is 0)
   int ctx, nd;
   bool bad;
   unit_lengths(a, u, ctx, nd, bad);
-  if (t >= nd) return;
-  const int first = a.unit_first[u], c0 = first >> 1, n = a.unit_last[u] - c0 + 1;
+  pdl_launch_dependents();
+  if (tile * a.tile_tokens >= nd) return;
+  const int c0 = first >> 1, n = last - c0 + 1;
   if (n == 1) return;                                        // written by the CTA that had the whole unit
-  const int row = t * a.geo.g + (h - kv * a.geo.g), rb = row / kRows, r = row - rb * kRows;
-  auto part = [&](int i) {
-    return ((long long)((c0 + i) * a.row_blocks + rb) * 2 + (i == 0 ? first & 1 : 0)) * kRows + r;
-  };
-  float M = -INFINITY;
-  for (int i = lane; i < n; i += 32) M = fmaxf(M, __ldcg(a.part_ml + part(i)).x);
+  const bool here = in_tile < a.tile_tokens * g && t < nd;
+  const int rb = tile / kQTiles, r = tile % kQTiles * kTile + min(in_tile, kTile - 1);
+  float M = -INFINITY, sum = 0.f;
+  float4 o[4];
 #pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
-  const float ref = M == -INFINITY ? 0.f : M;
-  float sum = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i0 = 0; i0 < n; i0 += 32) {
-    const float2 ml = i0 + lane < n ? __ldcg(a.part_ml + part(i0 + lane)) : make_float2(-INFINITY, 0.f);
-    const float w = exp2_fast(ml.x - ref);
-    sum += ml.y * w;
-    const int here = min(32, n - i0);
-    for (int i = 0; i < here; i += 8) {
-      float4 v[8];
+  for (int z = 0; z < 4; ++z) o[z] = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int kAhead = 3;
+  for (int i0 = split; here && i0 < n; i0 += kSplit * kAhead) {
+    float2 ml[kAhead];
+    float4 v[kAhead][4];
 #pragma unroll
-      for (int z = 0; z < 8; ++z)
-        v[z] = i + z < here ? __ldcg(reinterpret_cast<const float4*>(a.part_o + part(i0 + i + z) * kHeadDim) + lane)
-                            : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < kAhead; ++i) {
+      const int c = i0 + i * kSplit;
+      ml[i] = make_float2(-INFINITY, 0.f);
+      if (c < n) {
+        const long long p = (long long)((c0 + c) * a.row_blocks + rb) * 2 + (c == 0 ? first & 1 : 0);
+        ml[i] = __ldcg(a.part_ml + p * kRows + r);
 #pragma unroll
-      for (int z = 0; z < 8; ++z) {
-        const float wz = __shfl_sync(0xFFFFFFFFu, w, (i + z) & 31);
-        if (i + z < here) {
-          o.x = fmaf(v[z].x, wz, o.x); o.y = fmaf(v[z].y, wz, o.y); o.z = fmaf(v[z].z, wz, o.z); o.w = fmaf(v[z].w, wz, o.w);
-        }
+        for (int z = 0; z < 4; ++z) v[i][z] = __ldcg(a.part_o + (p * 32 + col * 4 + z) * kRows + r);
+      }
+    }
+    float top = M;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) top = fmaxf(top, ml[i].x);
+    const float ref = top == -INFINITY ? 0.f : top, keep = exp2_fast(M - ref);
+    M = top;
+    sum *= keep;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) { o[z].x *= keep; o[z].y *= keep; o[z].z *= keep; o[z].w *= keep; }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (i0 + i * kSplit >= n) break;
+      const float w = exp2_fast(ml[i].x - ref);
+      sum = fmaf(ml[i].y, w, sum);
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        o[z].x = fmaf(v[i][z].x, w, o[z].x); o[z].y = fmaf(v[i][z].y, w, o[z].y);
+        o[z].z = fmaf(v[i][z].z, w, o[z].z); o[z].w = fmaf(v[i][z].w, w, o[z].w);
       }
     }
   }
+  if constexpr (kSplit > 1) {
+    s_ml[split * 64 + lane] = M;
+    s_ml[split * 64 + 32 + lane] = sum;
 #pragma unroll
-  for (int s = 16; s >= 1; s >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
-  const __nv_bfloat162 lo = __floats2bfloat162_rn(o.x * inv, o.y * inv), hi = __floats2bfloat162_rn(o.z * inv, o.w * inv);
-  reinterpret_cast<uint2*>(a.out + at * kHeadDim)[lane] =
-      make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-  if (lane == 0) a.lse[at] = sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
+    for (int z = 0; z < 4; ++z) {
+      s_o[(split * 16 + 4 * z) * 32 + lane] = o[z].x;
+      s_o[(split * 16 + 4 * z + 1) * 32 + lane] = o[z].y;
+      s_o[(split * 16 + 4 * z + 2) * 32 + lane] = o[z].z;
+      s_o[(split * 16 + 4 * z + 3) * 32 + lane] = o[z].w;
+    }
+    __syncthreads();
+    // two coordinates per warp
+    static_assert(kSplit == 8, "16 coordinates over 8 warps");
+    M = s_ml[lane];
+#pragma unroll
+    for (int i = 1; i < kSplit; ++i) M = fmaxf(M, s_ml[i * 64 + lane]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    sum = 0.f;
+    float o0 = 0.f, o1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSplit; ++i) {
+      const float w = exp2_fast(s_ml[i * 64 + lane] - ref);
+      sum = fmaf(s_ml[i * 64 + 32 + lane], w, sum);
+      o0 = fmaf(s_o[(i * 16 + 2 * warp) * 32 + lane], w, o0);
+      o1 = fmaf(s_o[(i * 16 + 2 * warp + 1) * 32 + lane], w, o1);
+    }
+    if (!here) return;
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const long long at = ((long long)b * a.T + t) * a.geo.Hq + kv * g + h;
+    *reinterpret_cast<__nv_bfloat162*>(a.out + at * kHeadDim + col * 16 + 2 * warp) = __floats2bfloat162_rn(o0 * inv, o1 * inv);
+    if (warp == 0 && col == 0) a.lse[at] = sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
+  } else {
+    if (!here) return;
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const long long at = ((long long)b * a.T + t) * a.geo.Hq + kv * g + h;
+#pragma unroll
+    for (int z = 0; z < 4; z += 2) {
+      const __nv_bfloat162 w[4] = {__floats2bfloat162_rn(o[z].x * inv, o[z].y * inv), __floats2bfloat162_rn(o[z].z * inv, o[z].w * inv),
+                                   __floats2bfloat162_rn(o[z + 1].x * inv, o[z + 1].y * inv), __floats2bfloat162_rn(o[z + 1].z * inv, o[z + 1].w * inv)};
+      *reinterpret_cast<uint4*>(a.out + at * kHeadDim + col * 16 + z * 4) = *reinterpret_cast<const uint4*>(w);
+    }
+    if (col == 0) a.lse[at] = sum > 0.f ? (M + log2f(sum)) * kLn2 : -INFINITY;
+  }
 }
 
 // The pages that the heads of a KV head have selected, ascending, each with the heads that did: a CTA per unit.  The
@@ -969,7 +1042,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 EncodeTiledFn g_encode = nullptr;
 
-// bf16 tensor of five dimensions, the first of 64 coordinates, boxes with the 128-byte swizzle.  Strides in bytes.
+// bf16 tensor of five dimensions, boxes of 64 coordinates with the 128-byte swizzle.  Strides in bytes.
 cudaError_t make_map(CUtensorMap* map, const void* base, const cuuint64_t (&dims)[5], const cuuint64_t (&strides)[4], const cuuint32_t (&box)[5]) {
   if (g_encode == nullptr) return cudaErrorNotSupported;
   const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
@@ -985,11 +1058,13 @@ struct TreeLayout {
   int64_t part_o, part_ml, unit_first, unit_last, list, list_tokens, total;
   int list_cap;
 };
+int tile_tokens_of(const Geometry& geo) { return kTile / geo.g; }
+int row_tiles_of(const Geometry& geo, int T) { return (T + tile_tokens_of(geo) - 1) / tile_tokens_of(geo); }
 TreeLayout tree_layout(const Geometry& geo, int T) {
   TreeLayout l;
-  const int64_t units = (int64_t)geo.B * geo.Hkv, rows_all = (int64_t)T * geo.g;
-  const int64_t rows = rows_all > kTile ? 2 * kTile : kTile;
-  const int64_t ctas = std::max<int64_t>(kMaxTreeCtas, (rows_all + rows - 1) / rows);
+  const int64_t units = (int64_t)geo.B * geo.Hkv, tiles = row_tiles_of(geo, T);
+  const int64_t rows = tiles > 1 ? 2 * kTile : kTile;
+  const int64_t ctas = std::max<int64_t>(kMaxTreeCtas, (tiles + 1) / 2);
   l.list_cap = (int)std::min<int64_t>((int64_t)geo.g * geo.k, geo.Pmax);
   l.part_o = 0;
   l.part_ml = align256(l.part_o + ctas * 2 * rows * kHeadDim * 4);
@@ -1004,7 +1079,8 @@ TreeLayout tree_layout(const Geometry& geo, int T) {
 }  // namespace
 
 bool tree_supported(const Geometry& geo, int T, bool selected) {
-  if ((int64_t)T * geo.g >= (int64_t(1) << 30) || geo.n_pool_pages >= (int64_t(1) << 31) || (int64_t)geo.B * T * geo.Hq >= (int64_t(1) << 33))
+  if (geo.g > kTile || (int64_t)T * geo.g >= (int64_t(1) << 30) || geo.n_pool_pages >= (int64_t(1) << 31) || (int64_t)geo.B * geo.Hkv * row_tiles_of(geo, T) * 32 >= (int64_t(1) << 31) ||
+      (geo.n_pool_pages * geo.S / kTile + (int64_t)geo.B * (T / kTile + 2)) * geo.Hkv >= (int64_t(1) << 31))
     return false;
   return !selected || (geo.g <= 32 && (geo.Pmax + 31) / 32 * 8 <= kMaxTreeMapBytes);
 }
@@ -1035,7 +1111,8 @@ cudaError_t launch_tree_attn(const Geometry& geo, const TreeCall& c, void* works
   a.mask = c.mask;
   a.T = c.T;
   a.words = (c.T + 31) / 32;
-  a.part_o = reinterpret_cast<float*>(ws + lay.part_o);
+  a.part_o = reinterpret_cast<float4*>(ws + lay.part_o);
+  a.tile_tokens = tile_tokens_of(geo);
   a.part_ml = reinterpret_cast<float2*>(ws + lay.part_ml);
   a.unit_first = reinterpret_cast<int32_t*>(ws + lay.unit_first);
   a.unit_last = reinterpret_cast<int32_t*>(ws + lay.unit_last);
@@ -1046,7 +1123,7 @@ cudaError_t launch_tree_attn(const Geometry& geo, const TreeCall& c, void* works
 
   const cuuint64_t row = kHeadDim * 2, S = (cuuint64_t)geo.S, Hkv = (cuuint64_t)geo.Hkv, T = (cuuint64_t)c.T;
   // pool: (64 coordinates, token of the page, page, half of the coordinates, KV head and K or V)
-  CUtensorMap tile, page, dk, dv;
+  CUtensorMap tile, page, dk, dv, dq;
   const cuuint64_t pool_dims[5] = {64, S, (cuuint64_t)geo.n_pool_pages, 2, Hkv * 2};
   const cuuint64_t pool_strides[4] = {row, Hkv * 2 * S * row, 128, S * row};
   const cuuint32_t tile_box[5] = {64, (cuuint32_t)S, (cuuint32_t)(kTile / S), 2, 1}, page_box[5] = {64, (cuuint32_t)S, 1, 1, 1};
@@ -1058,6 +1135,11 @@ cudaError_t launch_tree_attn(const Geometry& geo, const TreeCall& c, void* works
   const cuuint32_t draft_box[5] = {64, (cuuint32_t)kTile, 2, 1, 1};
   if (e == cudaSuccess) e = make_map(&dk, c.k, draft_dims, draft_strides, draft_box);
   if (e == cudaSuccess) e = make_map(&dv, c.v, draft_dims, draft_strides, draft_box);
+  // queries: (128 coordinates, head of the group, token, KV head, request)
+  const cuuint64_t q_dims[5] = {kHeadDim, (cuuint64_t)geo.g, T, Hkv, (cuuint64_t)geo.B};
+  const cuuint64_t q_strides[4] = {row, (cuuint64_t)geo.Hq * row, (cuuint64_t)geo.g * row, T * (cuuint64_t)geo.Hq * row};
+  const cuuint32_t q_box[5] = {64, (cuuint32_t)geo.g, (cuuint32_t)a.tile_tokens, 1, 1};
+  if (e == cudaSuccess) e = make_map(&dq, c.q, q_dims, q_strides, q_box);
   if (e != cudaSuccess) return e;
 
   if (c.sel != nullptr) {
@@ -1069,19 +1151,21 @@ cudaError_t launch_tree_attn(const Geometry& geo, const TreeCall& c, void* works
     a.list = list;
     a.list_tokens = tokens;
   }
-  const int64_t rows = (int64_t)c.T * geo.g;
-  const bool wide = rows > kTile;
-  a.row_blocks = wide ? (int)((rows + 2 * kTile - 1) / (2 * kTile)) : 1;
+  const int tiles = row_tiles_of(geo, c.T);
+  const bool wide = tiles > 1;
+  a.row_blocks = (tiles + 1) / 2;
   const int64_t most = (int64_t)geo.B * geo.Hkv * (((int64_t)geo.Pmax * geo.S + kTile - 1) / kTile + (c.T + kTile - 1) / kTile);
   a.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kMaxTreeCtas, sm_count()) / a.row_blocks, most));
   const unsigned grid = (unsigned)(a.chunks * a.row_blocks);
-  e = wide ? launch_pdl(tree_attn_kernel<true>, dim3(grid), dim3(kThreads), (size_t)Layout<true>::kBytes, st, true, tile, page, dk, dv, a)
-           : launch_pdl(tree_attn_kernel<false>, dim3(grid), dim3(kThreads), (size_t)Layout<false>::kBytes, st, true, tile, page, dk, dv, a);
+  e = wide ? launch_pdl(tree_attn_kernel<true>, dim3(grid), dim3(kThreads), (size_t)Layout<true>::kBytes, st, true, tile, page, dk, dv, dq, a)
+           : launch_pdl(tree_attn_kernel<false>, dim3(grid), dim3(kThreads), (size_t)Layout<false>::kBytes, st, true, tile, page, dk, dv, dq, a);
   if (e != cudaSuccess) return e;
-  const int64_t out_rows = (int64_t)geo.B * c.T * geo.Hq;
-  const dim3 merge_grid((unsigned)((out_rows + 7) / 8));
-  return wide ? launch_pdl(tree_merge_kernel<2 * kTile>, merge_grid, dim3(256), 0, st, true, a)
-              : launch_pdl(tree_merge_kernel<kTile>, merge_grid, dim3(256), 0, st, true, a);
+  const int groups = (std::min(c.T, a.tile_tokens) * geo.g + 31) / 32;
+  // few units are cut into many parts: their partials are shared by the warps of a CTA
+  const bool many = (int64_t)geo.B * geo.Hkv * 4 <= a.chunks;
+  const dim3 merge_grid((unsigned)((int64_t)geo.B * geo.Hkv * tiles * groups * (many ? 8 : 1)));
+  auto* merge = wide ? (many ? tree_merge_kernel<2, 8> : tree_merge_kernel<2, 1>) : (many ? tree_merge_kernel<1, 8> : tree_merge_kernel<1, 1>);
+  return launch_pdl(merge, merge_grid, dim3(256), 0, st, true, a, groups, tiles);
 }
 
 }  // namespace swarm
