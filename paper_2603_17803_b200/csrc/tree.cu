@@ -461,19 +461,11 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         const Seg s = list[i];
         if (row_tiles(s.nd) <= 0) continue;
         const int n = s.t1 - s.t0;
-        if (kWide && row_tiles(s.nd) > 1) {
-          ok = load_tile(s, s.t0, 0);
-          for (int t = 0; ok && t < n; ++t) {
-            ok = load_tile(s, s.t0 + t, 1);
-            if (ok && t + 1 < n) ok = load_tile(s, s.t0 + t + 1, 0);
-          }
-        } else {
-          ok = load_tile(s, s.t0, 0);
-          if (ok && n > 1) ok = load_tile(s, s.t0 + 1, 0);
-          for (int t = 0; ok && t < n; ++t) {
-            ok = load_tile(s, s.t0 + t, 1);
-            if (ok && t + 2 < n) ok = load_tile(s, s.t0 + t + 2, 0);
-          }
+        // K of a tile, and V of the one that many tiles earlier whose softmax is done by then
+        const int behind = kWide && row_tiles(s.nd) > 1 ? 1 : 2;
+        for (int k = 0; ok && k < 2 * (n + behind); ++k) {
+          const int which = (k & 1) ^ 1, t = (k >> 1) - which * behind;
+          if (t >= 0 && t < n) ok = load_tile(s, s.t0 + t, which);
         }
       }
       });
@@ -532,77 +524,42 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         q_phase ^= 1u;
         if (!ok) break;
         tc_fence_after();
-        int sl;
-        unsigned ph;
-        if (wide) {
-          place(0, sl, ph);
-          if (!(ok = bar_wait(full + sl, ph, stop))) break;
-          scores(0, sl, 0);
-          commit(s_full);
-          scores(1, sl, 1);
-          commit(s_full + 1);
-          commit(empty + sl);
-          if (n == 1) commit(q_empty);
-          advance(1);
-          for (int t = 0; ok && t < n; ++t) {
-            int sv, sk;
-            unsigned pv, pk;
-            place(0, sv, pv);
-            place(1, sk, pk);
-            if (!(ok = bar_wait(full + sv, pv, stop))) break;
-            clear_tail(s, s.t0 + t, sv);
-#pragma unroll
-            for (int st = 0; st < 2; ++st) {
-              if (ok) ok = bar_wait(p_full + st, (p_phase >> st) & 1u, stop);
-              p_phase ^= 1u << st;
-              if (!ok) break;
-              tc_fence_after();
-              values(st, sv, t > 0);
-              if (st == 1) commit(empty + sv);
-              if (t + 1 < n) {
-                if (st == 0 && !(ok = bar_wait(full + sk, pk, stop))) break;
-                scores(st, sk, st);
-                if (st == 1) commit(empty + sk);
-                if (st == 1 && t + 2 == n) commit(q_empty);
-              }
-              commit(t + 1 < n ? s_full + st : o_full + st);
+        // Wide: both streams use every tile, step by step in turn: O += P V of a tile, then S of the next.  Else the streams take
+        // alternate tiles: O += P V of a tile, then S of the one after the next.
+        const int steps = wide ? 2 * n + 2 : n + 2;
+#pragma unroll 1
+        for (int j = 0; j < steps; ++j) {
+          const int st = j & 1, tv = wide ? (j >> 1) - 1 : j - 2, tk = wide ? j >> 1 : j;
+          const bool has_v = tv >= 0 && tv < n, has_k = tk < n;
+          const bool opens = !wide || st == 0, closes = !wide || st == 1;   // the first and the last use of the tiles
+          int sv, sk;
+          unsigned pv, pk;
+          place(0, sv, pv);
+          place(has_v ? 1 : 0, sk, pk);
+          if (has_v) {
+            if (opens) {
+              if (!(ok = bar_wait(full + sv, pv, stop))) break;
+              clear_tail(s, s.t0 + tv, sv);
             }
-            advance(t + 1 < n ? 2 : 1);
-          }
-        } else {
-          for (int st = 0; ok && st < min(n, 2); ++st) {
-            place(0, sl, ph);
-            if (!(ok = bar_wait(full + sl, ph, stop))) break;
-            scores(st, sl, 0);
-            commit(s_full + st);
-            commit(empty + sl);
-            advance(1);
-          }
-          if (ok && n <= 2) commit(q_empty);
-          for (int t = 0; ok && t < n; ++t) {
-            const int st = t & 1;
-            place(0, sl, ph);
-            if (!(ok = bar_wait(full + sl, ph, stop))) break;
-            clear_tail(s, s.t0 + t, sl);
             ok = bar_wait(p_full + st, (p_phase >> st) & 1u, stop);
             p_phase ^= 1u << st;
             if (!ok) break;
             tc_fence_after();
-            values(st, sl, t > 1);
-            commit(empty + sl);
-            advance(1);
-            if (t + 2 < n) {
-              place(0, sl, ph);
-              if (!(ok = bar_wait(full + sl, ph, stop))) break;
-              scores(st, sl, 0);
-              commit(s_full + st);
-              commit(empty + sl);
-              if (t + 3 == n) commit(q_empty);
-              advance(1);
-            } else {
-              commit(o_full + st);
-            }
+            values(st, sv, tv >= (wide ? 1 : 2));
+            if (closes) commit(empty + sv);
           }
+          if (has_k) {
+            if (opens && !(ok = bar_wait(full + sk, pk, stop))) break;
+            scores(st, sk, wide ? st : 0);
+            commit(s_full + st);
+            if (closes) {
+              commit(empty + sk);
+              if (tk == n - 1) commit(q_empty);
+            }
+          } else if (has_v) {
+            commit(o_full + st);
+          }
+          if (closes) advance((has_v ? 1 : 0) + (has_k ? 1 : 0));
         }
       }
       });
@@ -637,7 +594,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
     const float scale = 0.08838834764831845f * kLog2e;       // 1 / sqrt(128), in the log2 domain
     lists([&] {
       for (int i = 0; ok && i < count; ++i) {
-        const Seg s = list[i];
+        const Seg& s = list[i];                              // (read where it is needed: registers are short here)
         if (row_tiles(s.nd) <= 0) continue;
         const bool wide = kWide && row_tiles(s.nd) > 1;
         const int tile_first = (first_tile + (wide ? st : 0)) * a.tile_tokens;   // first token of this stream's rows
