@@ -59,7 +59,7 @@ static_assert(sizeof(Seg) == kSegIntsPerRow * 4, "listed as words");
 template <bool kWide>
 struct Layout {
   static constexpr int kQTiles = kWide ? 2 : 1;
-  static constexpr int kSlots = kWide ? 4 : 5;
+  static constexpr int kSlots = 4;                           // more leave too little L1 (6 and 5: up to 5 % slower)
   static constexpr int kRows = kQTiles * kTile;
   static constexpr int kRing = kQTiles * kTileBytes;
   static constexpr int kBars = kRing + kSlots * kTileBytes;
@@ -90,16 +90,15 @@ __device__ __forceinline__ bool bar_try(uint64_t* bar, unsigned parity) {
       : "memory");
   return ok != 0;
 }
-// Bounded wait of a whole warp.  When it runs out, `stop` tells the other warps of the CTA, whose waits then end as well;
-// the lanes agree on the answer.
+// Bounded wait of a whole warp, in step: branches that the lanes take together cost a fraction of diverging ones.  When it runs
+// out, `stop` tells the other warps of the CTA, whose waits then end as well.
 __device__ __forceinline__ bool bar_wait(uint64_t* bar, unsigned parity, volatile int* stop) {
-  bool there = false;
   for (unsigned polls = 0; polls < kWaitLimit; ++polls) {
-    there = bar_try(bar, parity);
-    if (there || *stop != 0) break;
+    if (__all_sync(0xFFFFFFFFu, bar_try(bar, parity))) return true;
+    if (__any_sync(0xFFFFFFFFu, *stop != 0)) return false;
   }
-  if (!there) *stop = 1;
-  return __all_sync(0xFFFFFFFFu, there);
+  *stop = 1;
+  return false;
 }
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, int c4, uint64_t* bar) {
   asm volatile(
@@ -135,8 +134,20 @@ __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+// Products and their commits are issued by one lane (`lead` = 1 there, else 0), as predicated instructions of a warp in step: in
+// a branch of its own for that lane their operands would not be known to be uniform, and each would take 100 cycles to issue.
+__device__ __forceinline__ uint32_t lead_lane() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p;
+}
+__device__ __forceinline__ void tc_commit(uint64_t* bar, uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_addr(bar)),
+      "r"(lead)
+      : "memory");
 }
 // Shared-memory operand with the 128-byte swizzle: `lead` and `stride` in bytes.
 __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead, uint32_t stride) {
@@ -146,28 +157,23 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead, uint32
 __host__ __device__ constexpr uint32_t mma_shape(bool transposed) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (transposed ? 1u << 16 : 0u) | ((uint32_t)(kTile / 8) << 17) | ((uint32_t)(kTile / 16) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add, uint32_t lead) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add), "r"(lead)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add, uint32_t lead) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add)
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add), "r"(lead)
       : "memory");
-}
-// True in one lane of the warp.  With a condition on the lane's number instead, the operands of a product are not known to be
-// uniform and move to uniform registers one by one: 100 cycles to issue each.
-__device__ __forceinline__ bool one() {
-  uint32_t p;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-  return p != 0;
 }
 __device__ __forceinline__ float exp2_fast(float x) {      // 2^x, relative error about 2^-22; 0 for x = -inf
   float y;
@@ -280,7 +286,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
   int* scan = reinterpret_cast<int*>(smem + L::kScan);
 
   const int tid = threadIdx.x, lane = tid & 31;
-  const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);    // (known to be the same for the whole warp: see `one`)
+  const int warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);    // (known to be the same for the whole warp: see lead_lane)
   const int rb = blockIdx.x % a.row_blocks, chunk = blockIdx.x / a.row_blocks;
   const int g = a.geo.g, Hkv = a.geo.Hkv, S = a.geo.S;
   const int units = a.geo.B * Hkv;
@@ -482,28 +488,23 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         ph = ring_phase;
         if (sl >= L::kSlots) { sl -= L::kSlots; ph ^= 1u; }
       };
+      const uint32_t lead = lead_lane();
       auto scores = [&](int st, int sl, int q_tile) {        // S = Q K^T
-        if (one()) {
-          const uint64_t qd = operand(q_at + q_tile * kTileBytes, 16, 1024);
-          const uint64_t kd = operand(smem_addr(smem + L::kRing + sl * kTileBytes), 16, 1024);
+        const uint64_t qd = operand(q_at + q_tile * kTileBytes, 16, 1024);
+        const uint64_t kd = operand(smem_addr(smem + L::kRing + sl * kTileBytes), 16, 1024);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const uint32_t off = (uint32_t)((k >> 2) * (kHalfBytes >> 4) + (k & 3) * 2);
-            mma_ss(tmem + st * kTile, qd + off, kd + off, mma_shape(false), k > 0);
-          }
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t off = (uint32_t)((k >> 2) * (kHalfBytes >> 4) + (k & 3) * 2);
+          mma_ss(tmem + st * kTile, qd + off, kd + off, mma_shape(false), k > 0, lead);
         }
       };
       auto values = [&](int st, int sl, bool add) {          // O += P V
-        if (one()) {
-          const uint64_t vd = operand(smem_addr(smem + L::kRing + sl * kTileBytes), kHalfBytes, 1024);
+        const uint64_t vd = operand(smem_addr(smem + L::kRing + sl * kTileBytes), kHalfBytes, 1024);
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            mma_ts(tmem + 256 + st * kTile, tmem + st * kTile + k * 8, vd + (uint64_t)(k * 128), mma_shape(true), add || k > 0);
-        }
+        for (int k = 0; k < 8; ++k)
+          mma_ts(tmem + 256 + st * kTile, tmem + st * kTile + k * 8, vd + (uint64_t)(k * 128), mma_shape(true), add || k > 0, lead);
       };
-      auto commit = [&](uint64_t* bar) {
-        if (one()) tc_commit(bar);
-      };
+      auto commit = [&](uint64_t* bar) { tc_commit(bar, lead); };
       // V rows behind the tile's last token may hold anything, and 0 * NaN must not reach the sums
       auto clear_tail = [&](const Seg& s, int t, int sl) {
         const int left = t < s.ctx_tiles ? s.ctx_tokens - t * kTile : s.nd - (t - s.ctx_tiles) * kTile;
@@ -806,7 +807,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
     if (warp == kQueryWarp && asked > 0)
       for (unsigned polls = 0; polls < kWaitLimit && !bar_try(q_full, (unsigned)(asked - 1) & 1u); ++polls) { }
     if (warp == kMmaWarp) {
-      if (one()) tc_commit(drained);
+      tc_commit(drained, lead_lane());
       for (unsigned polls = 0; polls < kWaitLimit && !bar_try(drained, 0u); ++polls) { }
     }
   }
