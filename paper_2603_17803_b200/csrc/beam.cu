@@ -77,6 +77,7 @@ __global__ void __launch_bounds__(kBeamThreads, kPer == 32 ? 3 : 4)
 beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__ keys, float2* __restrict__ sums) {
   constexpr int kVec = 16 / (int)sizeof(T), kVecs = kPer / kVec, kChunk = kBeamThreads * kPer;
   constexpr int kMany = 64;                                   // threads with a candidate that are gathered as they are
+  constexpr int kGather = 256;                                // candidates that are ranked together
   __shared__ key_t s_max[128];
   __shared__ key_t s_cand[kMaxBeamKeep + 128 * kPer];
   __shared__ key_t s_top[kMaxBeamKeep];
@@ -94,17 +95,21 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   const char* end = static_cast<const char*>(c.logits) + ((long long)(c.batch * c.n_beams - 1) * c.row_stride + V) * (int)sizeof(T);
   const int shift = (int)(reinterpret_cast<uintptr_t>(first) & 15u);
   auto whole = [&](int at) { return at + kVec <= V && first + (long long)at * (int)sizeof(T) + (shift ? 32 - shift : 16) <= end; };
+  // (every vector of a chunk that is not among the row's last ones)
+  auto inside = [&](int at0) { return at0 + kChunk <= V && first + (long long)(at0 + kChunk) * (int)sizeof(T) + 32 <= end; };
   uint4 raw[kVecs];
   auto fetch = [&](int at0) {
+    const bool all = inside(at0);
+    const char* p0 = first + ((long long)at0 + tid * kVec) * (int)sizeof(T) - shift;
+    if (shift == 0) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int at = at0 + (i * kBeamThreads + tid) * kVec;
-      if (!whole(at)) continue;
-      const char* p = first + (long long)at * (int)sizeof(T) - shift;
-      if (shift == 0) {
-        raw[i] = ldg_nc_v4(p);
-      } else {
-        const uint4 lo = __ldg(reinterpret_cast<const uint4*>(p)), hi = __ldg(reinterpret_cast<const uint4*>(p + 16));
+      for (int i = 0; i < kVecs; ++i)
+        if (all || whole(at0 + (i * kBeamThreads + tid) * kVec)) raw[i] = ldg_nc_v4(p0 + i * kBeamThreads * 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        if (!all && !whole(at0 + (i * kBeamThreads + tid) * kVec)) continue;
+        const uint4 lo = __ldg(reinterpret_cast<const uint4*>(p0 + i * kBeamThreads * 16)), hi = __ldg(reinterpret_cast<const uint4*>(p0 + i * kBeamThreads * 16 + 16));
         uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
         if (shift & 4) {
 #pragma unroll
@@ -123,18 +128,44 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   const int begin = stretch * span * kChunk, stop = min(V, begin + span * kChunk);
   if (tid == 0) s_count = 0;
   float top = -INFINITY, sum = 0.f;                           // of this thread's logits so far
-  float floor_ = -INFINITY;                                   // the least of the n_keep held, once there are as many
+  float floor_ = -INFINITY;                                   // the least of the n_keep largest at the last ranking
+  int held = 0;                                               // candidates gathered, at most
+  // Ranks the gathered candidates and keeps the n_keep largest.  Entered behind a barrier, left in front of one.
+  auto rank = [&] {
+    const int n = s_count;
+    if (n >= keep) {
+      for (int i = tid; i < n; i += kBeamThreads) {
+        const key_t k = s_cand[i];
+        int r = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) r += s_cand[j] > k;
+        if (r < keep) s_top[r] = k;
+      }
+      __syncthreads();
+      if (tid < keep) s_cand[tid] = s_top[tid];
+      if (tid == 0) s_count = keep;
+      floor_ = key_value(s_top[keep - 1]);
+      held = keep;
+    } else {
+      held = n;
+    }
+  };
   fetch(begin);
   for (int at0 = begin; at0 < stop; at0 += kChunk) {
     float x[kPer];
+    if (inside(at0)) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int at = at0 + (i * kBeamThreads + tid) * kVec;
-      if (whole(at)) {
-        Element<T>::unpack(raw[i], x + i * kVec);
-      } else {
+      for (int i = 0; i < kVecs; ++i) Element<T>::unpack(raw[i], x + i * kVec);
+    } else {
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) x[i * kVec + e] = at + e < V ? Element<T>::one(first, at + e) : -INFINITY;
+      for (int i = 0; i < kVecs; ++i) {
+        const int at = at0 + (i * kBeamThreads + tid) * kVec;
+        if (whole(at)) {
+          Element<T>::unpack(raw[i], x + i * kVec);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) x[i * kVec + e] = at + e < V ? Element<T>::one(first, at + e) : -INFINITY;
+        }
       }
     }
     if (at0 + kChunk < stop) fetch(at0 + kChunk);             // the next chunk is on its way meanwhile
@@ -154,6 +185,7 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
     for (int e = 0; e < kPer; ++e) part[e & 3] += exp_fast(x[e] - ref);
     sum += (part[0] + part[1]) + (part[2] + part[3]);
 
+    // Candidates: logits above the floor.  They are ranked, and the floor raised, when enough have come together.
     const bool hit = mine > floor_;
     const int hits = __syncthreads_count(hit);
     if (hits == 0) continue;
@@ -161,6 +193,10 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
     key_t bound = 0;
     float bound_value = -INFINITY;
     if (hits > kMany) {
+      if (held > keep) {                                      // (the bound below may bring as many as fit beside n_keep)
+        rank();
+        __syncthreads();
+      }
       const int group = keep > 32 ? 2 : 4, groups = kBeamThreads / group;
       int where = 0;
 #pragma unroll
@@ -186,8 +222,16 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
       __syncthreads();
       bound = s_bound;
       bound_value = key_value(bound);
+      held = kGather;                                         // (ranked below, whatever came)
+    } else {
+      int more = 0;                                           // candidates of this thread beyond its first
+      if (hit) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) more += x[e] > floor_;
+      }
+      held += hits + (kPer - 1) * __syncthreads_count(more > 1);
     }
-    if (hit && mine >= bound_value) {
+    if (mine > floor_ && mine >= bound_value) {
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {
         if (x[e] > floor_) {
@@ -196,21 +240,14 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
         }
       }
     }
-    __syncthreads();
-    const int n = s_count;
-    if (n < keep) continue;                                   // (the next writes are behind the next barrier)
-    for (int i = tid; i < n; i += kBeamThreads) {
-      const key_t k = s_cand[i];
-      int rank = 0;
-#pragma unroll 4
-      for (int j = 0; j < n; ++j) rank += s_cand[j] > k;
-      if (rank < keep) s_top[rank] = k;
+    if (held >= kGather) {
+      __syncthreads();
+      rank();
     }
-    __syncthreads();
-    if (tid < keep) s_cand[tid] = s_top[tid];
-    if (tid == 0) s_count = keep;
-    floor_ = key_value(s_top[keep - 1]);
   }
+  __syncthreads();
+  if (s_count > keep) rank();
+  __syncthreads();
   // the threads' sums
   float m = top;
 #pragma unroll
