@@ -22,7 +22,7 @@ namespace swarm {
 namespace {
 
 constexpr int kBeamThreads = 256;
-constexpr int kMergeThreads = 512;
+constexpr int kMergeThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 
 typedef unsigned long long key_t;
@@ -64,11 +64,56 @@ template <> struct Element<__half> {
   }
 };
 
-// 2^(t * log2 e) for t <= 0, the constant in two parts: the sums of different beams are compared far below 2^-24 of the exponent.
-__device__ __forceinline__ float exp_fast(float t) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaf(t, 1.9259629911e-8f, t * kLog2e)));
-  return y;
+constexpr float kLog2eLow = 1.9259629911e-8f;               // log2 e - kLog2e: sums of different beams are compared far below 2^-24
+__device__ __forceinline__ float exp2_fast(float y) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {   // NaN is passed over
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// Two floats in a register pair: one instruction for both.
+typedef unsigned long long pair_t;
+__device__ __forceinline__ pair_t pair_of(float lo, float hi) {
+  pair_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair(pair_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ pair_t fma2(pair_t a, pair_t b, pair_t c) {
+  pair_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ pair_t add2(pair_t a, pair_t b) {
+  pair_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ pair_t mul2(pair_t a, pair_t b) {
+  pair_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float exp_fast(float t) { return exp2_fast(fmaf(t, kLog2eLow, t * kLog2e)); }   // e^t for t <= 0
+// sum of e^(x - ref) over the logits, all <= ref (the difference first: logits of the type's lowest value mask, too)
+template <int n>
+__device__ __forceinline__ float sum_exp(const float (&x)[n], float ref) {
+  const pair_t l = pair_of(kLog2e, kLog2e), low = pair_of(kLog2eLow, kLog2eLow), r = pair_of(-ref, -ref);
+  pair_t part[2] = {0ull, 0ull};
+#pragma unroll
+  for (int e = 0; e < n; e += 2) {
+    const pair_t t = add2(pair_of(x[e], x[e + 1]), r);
+    float y0, y1;
+    unpair(fma2(t, low, mul2(t, l)), y0, y1);
+    part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], pair_of(exp2_fast(y0), exp2_fast(y1)));
+  }
+  float a, b;
+  unpair(add2(part[0], part[1]), a, b);
+  return a + b;
 }
 
 // A chunk is kPer tokens for each of kBeamThreads threads; a CTA takes `span` chunks of a row one after the other.
@@ -77,7 +122,6 @@ __global__ void __launch_bounds__(kBeamThreads, kPer == 32 ? 3 : 4)
 beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__ keys, float2* __restrict__ sums) {
   constexpr int kVec = 16 / (int)sizeof(T), kVecs = kPer / kVec, kChunk = kBeamThreads * kPer;
   constexpr int kMany = 64;                                   // threads with a candidate that are gathered as they are
-  constexpr int kGather = 256;                                // candidates that are ranked together
   __shared__ key_t s_max[128];
   __shared__ key_t s_cand[kMaxBeamKeep + 128 * kPer];
   __shared__ key_t s_top[kMaxBeamKeep];
@@ -89,6 +133,7 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int row = blockIdx.x / stretches, stretch = blockIdx.x - row * stretches;
   const int V = c.vocab, keep = c.n_keep;
+  const int gather = max(64, 2 * keep);                       // candidates that are ranked together (by comparing all with all)
   // Rows may start anywhere in a 16-byte line.  The tokens a thread has do not depend on that (equal rows give equal sums, and so
   // ties between beams stay ties): a vector across two lines is put together from both.
   const char* first = static_cast<const char*>(c.logits) + (long long)row * c.row_stride * (int)sizeof(T);
@@ -129,7 +174,6 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   if (tid == 0) s_count = 0;
   float top = -INFINITY, sum = 0.f;                           // of this thread's logits so far
   float floor_ = -INFINITY;                                   // the least of the n_keep largest at the last ranking
-  int held = 0;                                               // candidates gathered, at most
   // Ranks the gathered candidates and keeps the n_keep largest.  Entered behind a barrier, left in front of one.
   auto rank = [&] {
     const int n = s_count;
@@ -145,9 +189,6 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
       if (tid < keep) s_cand[tid] = s_top[tid];
       if (tid == 0) s_count = keep;
       floor_ = key_value(s_top[keep - 1]);
-      held = keep;
-    } else {
-      held = n;
     }
   };
   fetch(begin);
@@ -169,34 +210,37 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
       }
     }
     if (at0 + kChunk < stop) fetch(at0 + kChunk);             // the next chunk is on its way meanwhile
-    float mine = -INFINITY;
+    float best2[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      x[e] = fmaxf(x[e], -INFINITY);                          // NaN: never chosen
-      mine = fmaxf(mine, x[e]);
-    }
+    for (int e = 0; e < kPer; e += 2) best2[(e >> 1) & 1] = max3(best2[(e >> 1) & 1], x[e], x[e + 1]);
+    const float mine = fmaxf(best2[0], best2[1]);
     if (mine > top) {
       sum *= exp_fast(top - mine);                            // (0 * 2^-inf the first time)
       top = mine;
     }
     const float ref = top == -INFINITY ? 0.f : top;
-    float part[4] = {0.f, 0.f, 0.f, 0.f};
+    const float part = sum_exp(x, ref);
+    if (part == part) {
+      sum += part;
+    } else {                                                  // NaN among them: never chosen, counted as nothing
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) part[e & 3] += exp_fast(x[e] - ref);
-    sum += (part[0] + part[1]) + (part[2] + part[3]);
+      for (int e = 0; e < kPer; ++e) x[e] = fmaxf(x[e], -INFINITY);
+      sum += sum_exp(x, ref);
+    }
 
     // Candidates: logits above the floor.  They are ranked, and the floor raised, when enough have come together.
-    const bool hit = mine > floor_;
-    const int hits = __syncthreads_count(hit);
+    const int hits = __syncthreads_count(mine > floor_);
     if (hits == 0) continue;
+    const int held = s_count;
+    __syncthreads();
+    if (held >= (hits > kMany ? keep + 1 : gather)) {         // (many hits: the bound below may bring as many as fit beside n_keep)
+      rank();
+      __syncthreads();
+    }
     auto token = [&](int e) { return (uint32_t)(at0 + ((e / kVec) * kBeamThreads + tid) * kVec + e % kVec); };
     key_t bound = 0;
     float bound_value = -INFINITY;
     if (hits > kMany) {
-      if (held > keep) {                                      // (the bound below may bring as many as fit beside n_keep)
-        rank();
-        __syncthreads();
-      }
       const int group = keep > 32 ? 2 : 4, groups = kBeamThreads / group;
       int where = 0;
 #pragma unroll
@@ -222,27 +266,15 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
       __syncthreads();
       bound = s_bound;
       bound_value = key_value(bound);
-      held = kGather;                                         // (ranked below, whatever came)
-    } else {
-      int more = 0;                                           // candidates of this thread beyond its first
-      if (hit) {
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) more += x[e] > floor_;
-      }
-      held += hits + (kPer - 1) * __syncthreads_count(more > 1);
     }
-    if (mine > floor_ && mine >= bound_value) {
+    if (__any_sync(0xFFFFFFFFu, mine > floor_ && mine >= bound_value)) {
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {
-        if (x[e] > floor_) {
+        if (__any_sync(0xFFFFFFFFu, x[e] > floor_)) {
           const key_t k = make_key(x[e], token(e));
-          if (k >= bound) s_cand[atomicAdd(&s_count, 1)] = k;
+          if (x[e] > floor_ && k >= bound) s_cand[atomicAdd(&s_count, 1)] = k;
         }
       }
-    }
-    if (held >= kGather) {
-      __syncthreads();
-      rank();
     }
   }
   __syncthreads();
@@ -293,70 +325,86 @@ struct Cand {
 };
 __device__ __forceinline__ bool before(const Cand& a, const Cand& b) { return a.value > b.value || (a.value == b.value && a.index < b.index); }
 
+constexpr int kHold = 4;                                    // candidates that a thread keeps in registers
+
+// The candidates' sums are compared as ordered images with the index behind; what a thread cannot hold it reads again.
 __global__ void __launch_bounds__(kMergeThreads)
 beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restrict__ keys, const float2* __restrict__ sums) {
   extern __shared__ __align__(16) unsigned char smem[];
-  double* s_base = reinterpret_cast<double*>(smem);           // [n_beams] score - log sum exp
-  Cand* s_max = reinterpret_cast<Cand*>(s_base + c.n_beams);
+  double* s_base = reinterpret_cast<double*>(smem);           // [n_beams] log sum exp, then [n_beams] scores
+  double* s_score = s_base + c.n_beams;
+  Cand* s_max = reinterpret_cast<Cand*>(s_score + c.n_beams);
   Cand* s_cand = s_max + kMergeThreads;
   __shared__ Cand s_bound;
   __shared__ int s_count;
-  pdl_wait();
-  pdl_launch_dependents();
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int keep = c.n_keep, V = c.vocab;
+  const int per_beam = chunks * keep, total = c.n_beams * per_beam;
+  const key_t* list = keys + (long long)b * total;
+  pdl_wait();
+  pdl_launch_dependents();
+  key_t held[kHold];
+#pragma unroll
+  for (int i = 0; i < kHold; ++i) held[i] = tid + i * kMergeThreads < total ? list[tid + i * kMergeThreads] : 0;
+  for (int k = tid; k < c.n_beams; k += kMergeThreads) s_score[k] = (double)c.score[b * c.n_beams + k];
   for (int k = warp; k < c.n_beams; k += kMergeThreads / 32) {
     const float2* mine = sums + ((long long)b * c.n_beams + k) * chunks;
-    float m = -INFINITY;
-    for (int i = lane; i < chunks; i += 32) m = fmaxf(m, mine[i].x);
+    const float2 first = lane < chunks ? mine[lane] : make_float2(-INFINITY, 0.f);
+    float m = first.x;
+    for (int i = lane + 32; i < chunks; i += 32) m = fmaxf(m, mine[i].x);
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    double l = 0.0;
-    for (int i = lane; i < chunks; i += 32)
-      if (mine[i].x != -INFINITY) l += (double)mine[i].y * exp((double)mine[i].x - (double)m);
+    double l = first.x == -INFINITY ? 0.0 : (double)(first.y * exp_fast(first.x - m));
+    for (int i = lane + 32; i < chunks; i += 32)
+      if (mine[i].x != -INFINITY) l += (double)(mine[i].y * exp_fast(mine[i].x - m));
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
     if (lane == 0) s_base[k] = (double)m + log(l);            // (a beam without a finite logit offers no candidate)
   }
   if (tid == 0) s_count = 0;
   __syncthreads();
-  const int per_beam = chunks * keep, total = c.n_beams * per_beam;
-  const key_t* list = keys + (long long)b * total;
-  auto get = [&](int i) {
-    const key_t k = list[i];
+  auto cand = [&](int i, key_t k) {
     const int beam = i / per_beam;
     Cand r;
-    const double s = (double)c.score[b * c.n_beams + beam] + ((double)key_value(k) - s_base[beam]);
+    const double s = s_score[beam] + ((double)key_value(k) - s_base[beam]);
     r.value = k == 0 || !(s > -INFINITY) ? 0 : ordered(s + 0.0);
     r.index = (uint32_t)beam * (uint32_t)V + key_index(k);
     return r;
   };
-  Cand mine{0, 0xFFFFFFFFu - (uint32_t)tid};                  // (indices of their own, so that no two are equal)
-  for (int i = tid; i < total; i += kMergeThreads) {
-    const Cand r = get(i);
-    if (r.value != 0 && before(r, mine)) mine = r;
+  Cand mine[kHold], best{0, 0xFFFFFFFFu - (uint32_t)tid};     // (indices of their own, so that no two are equal)
+#pragma unroll
+  for (int i = 0; i < kHold; ++i) {
+    mine[i].value = 0;
+    if (tid + i * kMergeThreads < total) mine[i] = cand(tid + i * kMergeThreads, held[i]);
+    if (mine[i].value != 0 && before(mine[i], best)) best = mine[i];
+  }
+  for (int i = tid + kHold * kMergeThreads; i < total; i += kMergeThreads) {
+    const Cand r = cand(i, list[i]);
+    if (r.value != 0 && before(r, best)) best = r;
   }
   // maxima of groups of threads, where the candidates above their n_keep-th largest fit: ranking costs the square of their number
   for (int o = 1; o < group; o <<= 1) {
-    const Cand other{__shfl_xor_sync(0xFFFFFFFFu, mine.value, o), __shfl_xor_sync(0xFFFFFFFFu, mine.index, o)};
-    if (before(other, mine)) mine = other;
+    const Cand other{__shfl_xor_sync(0xFFFFFFFFu, best.value, o), __shfl_xor_sync(0xFFFFFFFFu, best.index, o)};
+    if (before(other, best)) best = other;
   }
-  if (tid % group == 0) s_max[tid / group] = mine;
+  if (tid % group == 0) s_max[tid / group] = best;
   __syncthreads();
-  if (tid < kMergeThreads / group) {
+  const int groups = kMergeThreads / group;
+  if (tid < groups) {
     const Cand max = s_max[tid];
     int above = 0;
 #pragma unroll 8
-    for (int i = 0; i < kMergeThreads / group; ++i) above += before(s_max[i], max);
+    for (int i = 0; i < groups; ++i) above += before(s_max[i], max);
     if (above == keep - 1) s_bound = max;
   }
   __syncthreads();
   const Cand bound = s_bound;
-  if (mine.value != 0 && !before(bound, mine)) {
-    for (int i = tid; i < total; i += kMergeThreads) {
-      const Cand r = get(i);
-      if (r.value != 0 && !before(bound, r)) s_cand[atomicAdd(&s_count, 1)] = r;
-    }
+#pragma unroll
+  for (int i = 0; i < kHold; ++i)
+    if (mine[i].value != 0 && !before(bound, mine[i])) s_cand[atomicAdd(&s_count, 1)] = mine[i];
+  for (int i = tid + kHold * kMergeThreads; i < total; i += kMergeThreads) {
+    const Cand r = cand(i, list[i]);
+    if (r.value != 0 && !before(bound, r)) s_cand[atomicAdd(&s_count, 1)] = r;
   }
   __syncthreads();
   const int n = s_count;
@@ -366,6 +414,7 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
     if (i < n) {
       r = s_cand[i];
       rank = 0;
+#pragma unroll 4
       for (int j = 0; j < n; ++j) rank += before(s_cand[j], r);
     }
     if (rank < keep) {
@@ -379,7 +428,8 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
 }
 
 // How a row is cut.  Elements per thread: 64 bytes of them (with the next 64 on their way), of 16-bit types 32 bytes where that
-// leaves SMs without a chunk.  Chunks per CTA: the first is the dear one, but about twelve CTAs per SM even out the waves.
+// leaves SMs without a chunk.  Chunks per CTA: as many as leave
+// three CTAs per SM, since the candidates grow rare with the length of a stretch.
 struct Cut {
   int per, span, stretches;
 };
@@ -387,7 +437,7 @@ Cut cut_of(long long rows, int vocab, int dtype) {
   Cut c;
   auto chunks = [&](int per) { return (vocab + kBeamThreads * per - 1) / (kBeamThreads * per); };
   c.per = dtype == SWARM_DTYPE_F32 || rows * chunks(32) < 148 ? 16 : 32;
-  c.span = (int)std::max<long long>(1, std::min<long long>(32, rows * chunks(c.per) / (148 * 12)));
+  c.span = (int)std::max<long long>(1, std::min<long long>(32, rows * chunks(c.per) / (148 * 3)));
   c.stretches = (chunks(c.per) + c.span - 1) / c.span;
   return c;
 }
@@ -395,7 +445,7 @@ constexpr int kMergeSmemMax = 200 * 1024;
 // Shared memory of the second kernel: every thread of the n_keep groups above the bound may bring all of its candidates.
 long long merge_smem(int beams, int chunks, int keep, int group) {
   const long long total = (long long)beams * chunks * keep, per = (total + kMergeThreads - 1) / kMergeThreads;
-  return beams * 8LL + (kMergeThreads + std::min(keep * per * group, total)) * (long long)sizeof(Cand);
+  return beams * 16LL + (kMergeThreads + std::min(keep * per * group, total)) * (long long)sizeof(Cand);
 }
 int merge_group(int beams, int chunks, int keep) { return merge_smem(beams, chunks, keep, 4) <= kMergeSmemMax ? 4 : 1; }
 
