@@ -116,6 +116,33 @@ __device__ __forceinline__ float sum_exp(const float (&x)[n], float ref) {
   return a + b;
 }
 
+// out(i, rank) for every i < n, rank = how many j < n have greater(j, i).  All threads take part; entered behind a barrier.  Where
+// there are more threads than entries, several share an entry's comparisons.
+template <int kThreads, class Greater, class Out>
+__device__ __forceinline__ void rank_all(int n, int* s_rank, Greater&& greater, Out&& out) {
+  const int tid = threadIdx.x;
+  if (2 * n > kThreads) {
+    for (int i = tid; i < n; i += kThreads) {
+      int r = 0;
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) r += greater(j, i);
+      out(i, r);
+    }
+    return;
+  }
+  const int width = n <= 32 ? 32 : 1 << (32 - __clz(n - 1)), parts = kThreads / width, i = tid & (width - 1);
+  if (tid < n) s_rank[tid] = 0;
+  __syncthreads();
+  if (i < n) {
+    int r = 0;
+#pragma unroll 4
+    for (int j = tid / width; j < n; j += parts) r += greater(j, i);
+    if (r != 0) atomicAdd(s_rank + i, r);
+  }
+  __syncthreads();
+  if (tid < n) out(tid, s_rank[tid]);
+}
+
 // A chunk is kPer tokens for each of kBeamThreads threads; a CTA takes `span` chunks of a row one after the other.
 template <class T, int kPer>
 __global__ void __launch_bounds__(kBeamThreads, kPer == 32 ? 3 : 4)
@@ -336,7 +363,7 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
   Cand* s_max = reinterpret_cast<Cand*>(s_score + c.n_beams);
   Cand* s_cand = s_max + kMergeThreads;
   __shared__ Cand s_bound;
-  __shared__ int s_count;
+  __shared__ int s_count, s_rank[kMergeThreads];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int keep = c.n_keep, V = c.vocab;
   const int per_beam = chunks * keep, total = c.n_beams * per_beam;
@@ -390,13 +417,7 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
   if (tid % group == 0) s_max[tid / group] = best;
   __syncthreads();
   const int groups = kMergeThreads / group;
-  if (tid < groups) {
-    const Cand max = s_max[tid];
-    int above = 0;
-#pragma unroll 8
-    for (int i = 0; i < groups; ++i) above += before(s_max[i], max);
-    if (above == keep - 1) s_bound = max;
-  }
+  rank_all<kMergeThreads>(groups, s_rank, [&](int j, int i) { return before(s_max[j], s_max[i]); }, [&](int i, int r) { if (r == keep - 1) s_bound = s_max[i]; });
   __syncthreads();
   const Cand bound = s_bound;
 #pragma unroll
@@ -408,23 +429,15 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
   }
   __syncthreads();
   const int n = s_count;
-  for (int i = tid; i < max(n, keep); i += kMergeThreads) {
-    int rank = i;
-    Cand r{0, 0};
-    if (i < n) {
-      r = s_cand[i];
-      rank = 0;
-#pragma unroll 4
-      for (int j = 0; j < n; ++j) rank += before(s_cand[j], r);
-    }
-    if (rank < keep) {
-      const long long at = (long long)b * keep + rank;
-      const bool some = r.value != 0;
-      c.new_score[at] = some ? (float)unordered_d(r.value) : -INFINITY;
-      c.parent[at] = some ? b * c.n_beams + (int)(r.index / (uint32_t)V) : -1;
-      c.token[at] = some ? (int)(r.index % (uint32_t)V) : -1;
-    }
-  }
+  auto write = [&](const Cand& r, int rank) {
+    const long long at = (long long)b * keep + rank;
+    const bool some = r.value != 0;
+    c.new_score[at] = some ? (float)unordered_d(r.value) : -INFINITY;
+    c.parent[at] = some ? b * c.n_beams + (int)(r.index / (uint32_t)V) : -1;
+    c.token[at] = some ? (int)(r.index % (uint32_t)V) : -1;
+  };
+  if (tid >= n && tid < keep) write(Cand{0, 0}, tid);
+  rank_all<kMergeThreads>(n, s_rank, [&](int j, int i) { return before(s_cand[j], s_cand[i]); }, [&](int i, int r) { if (r < keep) write(s_cand[i], r); });
 }
 
 // How a row is cut.  Elements per thread: 64 bytes of them (with the next 64 on their way), of 16-bit types 32 bytes where that
