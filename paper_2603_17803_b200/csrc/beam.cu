@@ -166,22 +166,19 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   const char* first = static_cast<const char*>(c.logits) + (long long)row * c.row_stride * (int)sizeof(T);
   const char* end = static_cast<const char*>(c.logits) + ((long long)(c.batch * c.n_beams - 1) * c.row_stride + V) * (int)sizeof(T);
   const int shift = (int)(reinterpret_cast<uintptr_t>(first) & 15u);
-  auto whole = [&](int at) { return at + kVec <= V && first + (long long)at * (int)sizeof(T) + (shift ? 32 - shift : 16) <= end; };
-  // (every vector of a chunk that is not among the row's last ones)
-  auto inside = [&](int at0) { return at0 + kChunk <= V && first + (long long)(at0 + kChunk) * (int)sizeof(T) + 32 <= end; };
+  const int begin = stretch * span * kChunk, stop = min(V, begin + span * kChunk);
+  // chunks of this stretch whose vectors (with the line behind, where they are put together) lie inside the row and the tensor
+  const int n_whole = max(0, (int)min((long long)(stop - begin), (long long)(end - 32 - first) / (int)sizeof(T) - begin) / kChunk);
+  const char* next = first + ((long long)begin + tid * kVec) * (int)sizeof(T) - shift;
   uint4 raw[kVecs];
-  auto fetch = [&](int at0) {
-    const bool all = inside(at0);
-    const char* p0 = first + ((long long)at0 + tid * kVec) * (int)sizeof(T) - shift;
+  auto fetch = [&] {
     if (shift == 0) {
 #pragma unroll
-      for (int i = 0; i < kVecs; ++i)
-        if (all || whole(at0 + (i * kBeamThreads + tid) * kVec)) raw[i] = ldg_nc_v4(p0 + i * kBeamThreads * 16);
+      for (int i = 0; i < kVecs; ++i) raw[i] = ldg_nc_v4(next + i * kBeamThreads * 16);
     } else {
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
-        if (!all && !whole(at0 + (i * kBeamThreads + tid) * kVec)) continue;
-        const uint4 lo = __ldg(reinterpret_cast<const uint4*>(p0 + i * kBeamThreads * 16)), hi = __ldg(reinterpret_cast<const uint4*>(p0 + i * kBeamThreads * 16 + 16));
+        const uint4 lo = __ldg(reinterpret_cast<const uint4*>(next + i * kBeamThreads * 16)), hi = __ldg(reinterpret_cast<const uint4*>(next + i * kBeamThreads * 16 + 16));
         uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
         if (shift & 4) {
 #pragma unroll
@@ -196,8 +193,8 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
                             __funnelshift_r(w[3], w[4], bits));
       }
     }
+    next += kChunk * (int)sizeof(T);
   };
-  const int begin = stretch * span * kChunk, stop = min(V, begin + span * kChunk);
   if (tid == 0) s_count = 0;
   float top = -INFINITY, sum = 0.f;                           // of this thread's logits so far
   float floor_ = -INFINITY;                                   // the least of the n_keep largest at the last ranking
@@ -218,25 +215,21 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
       floor_ = key_value(s_top[keep - 1]);
     }
   };
-  fetch(begin);
-  for (int at0 = begin; at0 < stop; at0 += kChunk) {
+  if (n_whole > 0) fetch();
+  for (int at0 = begin, chunk = 0; at0 < stop; at0 += kChunk, ++chunk) {
     float x[kPer];
-    if (inside(at0)) {
+    if (chunk < n_whole) {
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) Element<T>::unpack(raw[i], x + i * kVec);
+      if (chunk + 1 < n_whole) fetch();                       // the next chunk is on its way meanwhile
     } else {
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
         const int at = at0 + (i * kBeamThreads + tid) * kVec;
-        if (whole(at)) {
-          Element<T>::unpack(raw[i], x + i * kVec);
-        } else {
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) x[i * kVec + e] = at + e < V ? Element<T>::one(first, at + e) : -INFINITY;
-        }
+        for (int e = 0; e < kVec; ++e) x[i * kVec + e] = at + e < V ? Element<T>::one(first, at + e) : -INFINITY;
       }
     }
-    if (at0 + kChunk < stop) fetch(at0 + kChunk);             // the next chunk is on its way meanwhile
     float best2[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int e = 0; e < kPer; e += 2) best2[(e >> 1) & 1] = max3(best2[(e >> 1) & 1], x[e], x[e + 1]);
