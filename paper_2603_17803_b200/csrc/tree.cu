@@ -51,10 +51,8 @@ struct Seg {                                               // tiles [t0, t1) of 
   int ctx_tiles, ctx_tokens;
   int nd;                                                  // drafted tokens
   int last;                                                // t1 ends the unit
+  int base;                                                // first pool page of the request
 };
-
-constexpr int kSegIntsPerRow = 8;
-static_assert(sizeof(Seg) == kSegIntsPerRow * 4, "listed as words");
 
 template <bool kWide>
 struct Layout {
@@ -249,11 +247,12 @@ struct TreeArgs {
   uint32_t* status;
 };
 
-// Context tokens (those of the selected pages, if there is a selection) and drafted tokens of a unit; no drafted
+// Context tokens (those of the selected pages, if there is a selection), drafted tokens and first pool page of a unit; no drafted
 // tokens where the request's length does not fit its pages.
-__device__ __forceinline__ void unit_lengths(const TreeArgs& a, int u, int& ctx, int& nd, bool& bad) {
+__device__ __forceinline__ void unit_lengths(const TreeArgs& a, int u, int& ctx, int& nd, int& base, bool& bad) {
   const int b = u / a.geo.Hkv;
   const int len = a.ctx_len[b];
+  base = (int)a.page_base[b];
   const long long owned = a.page_base[b + 1] - a.page_base[b];
   nd = a.n_draft[b];
   bad = nd < 0 || nd > a.T;
@@ -313,17 +312,17 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
 
   // ---- this CTA's share of all tiles: the list of units is summed by the whole CTA, the unit of its first tile found.  Up to a
   // unit per thread, their lengths stay in shared memory (the ring is still empty) for the first list of segments.
-  int2* lengths = reinterpret_cast<int2*>(smem + L::kRing);
+  int4* lengths = reinterpret_cast<int4*>(smem + L::kRing);
   const bool cached = units <= kThreads;
   const int per = (units + kThreads - 1) / kThreads;
   const int u_lo = min(units, tid * per), u_hi = min(units, u_lo + per);
   int mine = 0;
   for (int u = u_lo; u < u_hi; ++u) {
-    int ctx, nd;
+    int ctx, nd, base;
     bool bad;
-    unit_lengths(a, u, ctx, nd, bad);
+    unit_lengths(a, u, ctx, nd, base, bad);
     if (bad && blockIdx.x == 0 && u % Hkv == 0) atomicOr(a.status, SWARM_DEV_BAD_LENGTH);
-    if (cached) lengths[u] = make_int2(ctx, nd);
+    if (cached) lengths[u] = make_int4(ctx, nd, base, 0);
     mine += tiles_of(ctx, nd);
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (in front of the copies that go there)
@@ -348,9 +347,9 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
   if (w0 < w1 && before <= w0 && w0 < before + mine) {       // one thread: its units hold the first tile
     int u = u_lo, at = before;
     for (; u + 1 < u_hi; ++u) {
-      int ctx, nd;
+      int ctx, nd, base;
       bool bad;
-      unit_lengths(a, u, ctx, nd, bad);
+      unit_lengths(a, u, ctx, nd, base, bad);
       const int n = tiles_of(ctx, nd);
       if (at + n > w0) break;
       at += n;
@@ -379,15 +378,16 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
       if (*stop != 0) break;
       if (warp == kListWarp) {                                   // the next (up to 32) units with tiles in this CTA's share
         const int u = u_next + lane;
-        int ctx = 0, nd = 0, n = 0;
+        int ctx = 0, nd = 0, base = 0, n = 0;
         bool bad;
         if (u < units) {
           if (cached && first_list) {
-            const int2 v = lengths[u];
+            const int4 v = lengths[u];
             ctx = v.x;
             nd = v.y;
+            base = v.z;
           } else {
-            unit_lengths(a, u, ctx, nd, bad);
+            unit_lengths(a, u, ctx, nd, base, bad);
           }
           n = tiles_of(ctx, nd);
         }
@@ -411,6 +411,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
           s.ctx_tokens = ctx;
           s.nd = nd;
           s.last = s.t1 == n;
+          s.base = base;
           list[__popc(all & ((1u << lane) - 1u))] = s;
           if (rb == 0) {
             if (s.t0 == 0) a.unit_first[u] = 2 * chunk + (begin == w0 ? 0 : 1);
@@ -433,7 +434,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");     // 128 * 72 + 256 * 216 = 384 * 168, what the CTA was launched with
     if (warp == kLoadWarp) {
       // ---- copies, in the order the matrix products use them
-      auto load_tile = [&](const Seg& s, int t, int which) -> bool {   // which: 0 = K, 1 = V
+      // which: 0 = K, 1 = V; `page`: the lane's page of the tile, where pages are selected
+      auto load_tile = [&](const Seg& s, int t, int which, int page) -> bool {
         if (issued >= L::kSlots && !bar_wait(empty + slot, ring_phase ^ 1u, stop)) return false;
         const uint32_t dst = smem_addr(smem + L::kRing + slot * kTileBytes);
         uint64_t* bar = full + slot;
@@ -445,17 +447,15 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         } else if (a.list == nullptr) {
           if (lane == 0) {
             bar_expect(bar, kTileBytes);
-            tma_load(dst, &pool_tile, 0, 0, (int)(a.page_base[s.b] + (long long)t * (kTile / S)), 0, s.kv * 2 + which, bar);
+            tma_load(dst, &pool_tile, 0, 0, s.base + t * (kTile / S), 0, s.kv * 2 + which, bar);
           }
         } else {                                             // the tile's pages one by one, a lane each
           const int per_tile = kTile / S, pages = min(per_tile, (s.ctx_tokens + S - 1) / S - t * per_tile);
           if (lane == 0) bar_expect(bar, (unsigned)(pages * S * kHeadDim * 2));
           __syncwarp();
-          if (lane < pages) {
-            const int page = (int)a.page_base[s.b] + a.list[(long long)(s.b * Hkv + s.kv) * a.list_cap + t * per_tile + lane].x;
+          if (lane < pages)
             for (int h = 0; h < 2; ++h)
-              tma_load(dst + h * kHalfBytes + lane * S * 128, &pool_page, 0, 0, page, h, s.kv * 2 + which, bar);
-          }
+              tma_load(dst + h * kHalfBytes + lane * S * 128, &pool_page, 0, 0, s.base + page, h, s.kv * 2 + which, bar);
         }
         __syncwarp();
         ++issued;
@@ -469,9 +469,16 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         const int n = s.t1 - s.t0;
         // K of a tile, and V of the one that many tiles earlier whose softmax is done by then
         const int behind = kWide && row_tiles(s.nd) > 1 ? 1 : 2;
+        // the list of pages is read a tile ahead: its latency would lie in front of every copy
+        const int per_tile = kTile / S, listed = a.list != nullptr ? (s.ctx_tokens + S - 1) / S : 0;
+        const int2* pages = a.list + (long long)(s.b * Hkv + s.kv) * a.list_cap + lane;
+        auto page_of = [&](int t) { return lane < per_tile && t * per_tile + lane < listed ? pages[t * per_tile].x : 0; };
+        int now = page_of(s.t0), next = 0, before = 0, before2 = 0;
         for (int k = 0; ok && k < 2 * (n + behind); ++k) {
           const int which = (k & 1) ^ 1, t = (k >> 1) - which * behind;
-          if (t >= 0 && t < n) ok = load_tile(s, s.t0 + t, which);
+          if (which == 1) next = page_of(s.t0 + (k >> 1) + 1);
+          if (t >= 0 && t < n) ok = load_tile(s, s.t0 + t, which, which == 0 ? now : behind == 1 ? before : before2);
+          if (which == 0) { before2 = before; before = now; now = next; }
         }
       }
       });
@@ -836,11 +843,12 @@ tree_merge_kernel(const TreeArgs a, int groups, int tiles) {
   const int tile = id % tiles, u = id / tiles;
   const int b = u / a.geo.Hkv, kv = u - b * a.geo.Hkv, g = a.geo.g;
   const int in_tile = group * 32 + lane, t = tile * a.tile_tokens + in_tile / g, h = in_tile % g;
+  // (the caller's tables: nothing between the wait of the kernel in front and here writes them)
+  const int len = a.ctx_len[b];
+  const long long owned = a.page_base[b + 1] - a.page_base[b];
+  const int nd = len < 0 || pages_of(len, a.geo.S) > owned ? 0 : max(0, min(a.n_draft[b], a.T));
   pdl_wait();
   const int first = a.unit_first[u], last = a.unit_last[u];  // (not written where nd is 0)
-  int ctx, nd;
-  bool bad;
-  unit_lengths(a, u, ctx, nd, bad);
   pdl_launch_dependents();
   if (tile * a.tile_tokens >= nd) return;
   const int c0 = first >> 1, n = last - c0 + 1;
