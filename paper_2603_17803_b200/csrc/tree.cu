@@ -612,37 +612,38 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         const int n = s.t1 - s.t0;
         const int my_n = wide ? n : (n + 1 - st) >> 1;
         float m = -INFINITY, l = 0.f;
+        // the heads that have selected the lane's page of a tile
+        auto heads_of = [&](int t) {
+          const int at = t * (kTile / S) + lane;
+          return lane < kTile / S && at * S < s.ctx_tokens && t < s.ctx_tiles ? a.list[(long long)(s.b * Hkv + s.kv) * a.list_cap + at].y : 0;
+        };
+        int heads_ahead = a.list != nullptr ? heads_of(s.t0 + (wide ? 0 : st)) : 0;
         for (int k = 0; k < my_n; ++k) {
           const int t = s.t0 + (wide ? k : 2 * k + st);
-          // which of the tile's tokens the row sees
-          uint32_t see[4] = {0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu};
-          const bool partial = a.list != nullptr || t >= s.ctx_tiles || (t + 1) * kTile > s.ctx_tokens;
-          if (busy && partial) {
-            const int first = (t < s.ctx_tiles ? t : t - s.ctx_tiles) * kTile;   // of the context or of the drafted tokens
-            const int left = (t < s.ctx_tiles ? s.ctx_tokens : s.nd) - first;
+          // Which of the tile's tokens the row sees: all; or whole pages, a bit per 16 tokens; or token by token.
+          const bool of_ctx = t < s.ctx_tiles;
+          const int first = (of_ctx ? t : t - s.ctx_tiles) * kTile, left = (of_ctx ? s.ctx_tokens : s.nd) - first;
+          const bool by_token = !of_ctx || left < kTile, by_page = a.list != nullptr && of_ctx;
+          uint32_t see[4] = {0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu, 0xFFFFFFFFu}, on = 0xFFu;
+          if (by_page) {
+            const int heads = heads_ahead;                   // of the lane's page; the next tile's are on their way meanwhile
+            heads_ahead = heads_of(t + (wide ? 1 : 2));
+            uint32_t bits = 0u;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) see[w] = left >= 32 * w + 32 ? 0xFFFFFFFFu : left > 32 * w ? (1u << (left - 32 * w)) - 1u : 0u;
-            if (t >= s.ctx_tiles) {
+            for (int p = 0; p < 8; ++p) bits |= ((uint32_t)__shfl_sync(0xFFFFFFFFu, heads, S == 16 ? p : p >> 1) >> h_row & 1u) << p;
+            on = bits;
+          }
+          if (busy && by_token) {
 #pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                const int at = first + 32 * w;
-                if (a.mask == nullptr)
-                  see[w] &= t_row >= at + 31 ? 0xFFFFFFFFu : t_row >= at ? (2u << (t_row - at)) - 1u : 0u;
-                else if (t_row < s.nd)
-                  see[w] &= at / 32 < a.words ? a.mask[((long long)s.b * a.T + t_row) * a.words + at / 32] : 0u;
-              }
-            } else if (a.list != nullptr) {
-              const int2* pages = a.list + (long long)(s.b * Hkv + s.kv) * a.list_cap + first / S;
-              const int n_pages = (left + S - 1) / S;
-#pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                if (S == 16) {
-                  const uint32_t lo = 2 * w < n_pages ? (uint32_t)pages[2 * w].y : 0u, hi = 2 * w + 1 < n_pages ? (uint32_t)pages[2 * w + 1].y : 0u;
-                  see[w] &= ((lo >> h_row) & 1u ? 0xFFFFu : 0u) | ((hi >> h_row) & 1u ? 0xFFFF0000u : 0u);
-                } else {
-                  see[w] &= w < n_pages && (((uint32_t)pages[w].y >> h_row) & 1u) ? 0xFFFFFFFFu : 0u;
-                }
-              }
+            for (int w = 0; w < 4; ++w) {
+              see[w] = left >= 32 * w + 32 ? 0xFFFFFFFFu : left > 32 * w ? (1u << (left - 32 * w)) - 1u : 0u;
+              const int at = first + 32 * w;
+              if (of_ctx)
+                see[w] &= ((on >> 2 * w) & 1u ? 0xFFFFu : 0u) | ((on >> 2 * w) & 2u ? 0xFFFF0000u : 0u);
+              else if (a.mask == nullptr)
+                see[w] &= t_row >= at + 31 ? 0xFFFFFFFFu : t_row >= at ? (2u << (t_row - at)) - 1u : 0u;
+              else if (t_row < s.nd)
+                see[w] &= at / 32 < a.words ? a.mask[((long long)s.b * a.T + t_row) * a.words + at / 32] : 0u;
             }
           }
           if (!(ok = bar_wait(s_full + st, s_phase, stop))) break;
@@ -653,19 +654,22 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
 #pragma unroll
             for (int w = 0; w < 4; ++w) tmem_ld32(x[w], s_at + 32 * w);
             tmem_wait_ld();
-            if (partial) {
+            if (by_token) {
 #pragma unroll
               for (int w = 0; w < 4; ++w)
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
                   if (!((see[w] >> e) & 1u)) x[w][e] = 0xFF800000u;   // -inf, whatever the padding held
             }
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            float top = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < 4; ++w)
+            for (int p = 0; p < 8; ++p) {
+              float mx = -INFINITY;
 #pragma unroll
-              for (int e = 0; e < 32; e += 2) mx[w] = max3(mx[w], __uint_as_float(x[w][e]), __uint_as_float(x[w][e + 1]));
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+              for (int e = 0; e < 16; e += 2) mx = max3(mx, __uint_as_float(x[p >> 1][16 * (p & 1) + e]), __uint_as_float(x[p >> 1][16 * (p & 1) + e + 1]));
+              top = fmaxf(top, (on >> p) & 1u ? mx : -INFINITY);
+            }
+            top *= scale;
             if (k == 0) {
               m = top;
             } else {
@@ -689,14 +693,16 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
             const float ref = m == -INFINITY ? 0.f : -m;
             // P is rounded to bf16 for the matrix product with V (half a step, 2^-8 of each weight at most); the sum keeps fp32
             pair_t sum[2] = {0ull, 0ull};
-            const pair_t scale2 = pair_of(scale, scale), ref2 = pair_of(ref, ref);
+            const pair_t scale2 = pair_of(scale, scale);
             auto weigh = [&](auto mixed) {
 #pragma unroll
               for (int w = 0; w < 4; ++w) {
                 uint32_t p[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                  const pair_t y = fma2(pair_of(__uint_as_float(x[w][2 * e]), __uint_as_float(x[w][2 * e + 1])), scale2, ref2);
+                  // (a page that the row's head has not selected: -inf in place of -m)
+                  const float r = decltype(mixed)::value || ((on >> (2 * w + (e >> 3))) & 1u) ? ref : -INFINITY;
+                  const pair_t y = fma2(pair_of(__uint_as_float(x[w][2 * e]), __uint_as_float(x[w][2 * e + 1])), scale2, pair_of(r, r));
                   float p0, p1;
                   if (decltype(mixed)::value && kByFma >> (e & 7) & 1) {
                     exp2_pair(y, p0, p1);
@@ -712,7 +718,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
                 tmem_st16(s_at + 16 * w, p);
               }
             };
-            if (partial) weigh(std::false_type());           // (-inf has to give 0)
+            if (by_token || by_page) weigh(std::false_type());   // (-inf has to give 0)
             else weigh(std::true_type());
             float s0, s1;
             unpair(add2(sum[0], sum[1]), s0, s1);
