@@ -188,6 +188,72 @@ class Session:
     def step_medoid(self, stream=None):
         B.swarm_step_medoid(self.ctx, self.inputs, self.medoid_index, self.medoid_outputs, stream)
 
+    # -- several continuations of a request ----------------------------------------------------------
+    def _allocated_for(self, stream, *tensors) -> None:
+        """Tensors just taken from the current stream's memory are about to be used on ``stream``."""
+        here = torch.cuda.current_stream(self.device)
+        if stream is not None and stream != here:
+            stream.wait_stream(here)
+            for t in tensors:
+                t.record_stream(stream)
+
+    def tree_attn(self, q, k, v, n_draft, mask=None, *, selected=False, out=None, lse=None, stream=None):
+        """swarm_tree_attn for drafted tokens q [B, T, Hq, d], k / v [B, T, Hkv, d]: over the whole context of every
+        request, or, with ``selected``, over the pages of the last select() / step().  Returns (out, lse)."""
+        cfg, T = self.cfg, q.shape[1]
+        for name, t, heads in (("q", q, cfg.n_q_heads), ("k", k, cfg.n_kv_heads), ("v", v, cfg.n_kv_heads)):
+            if tuple(t.shape) != (cfg.batch, T, heads, cfg.head_dim):
+                raise ValueError(f"{name} must have shape {(cfg.batch, T, heads, cfg.head_dim)}, not {tuple(t.shape)}")
+        rows = (cfg.batch, T, cfg.n_q_heads)
+        out = torch.zeros((*rows, cfg.head_dim), dtype=torch.bfloat16, device=self.device) if out is None else out
+        lse = torch.zeros(rows, dtype=torch.float32, device=self.device) if lse is None else lse
+        if tuple(out.shape) != (*rows, cfg.head_dim) or tuple(lse.shape) != rows:
+            raise ValueError("out and lse must have the shapes of q and of its rows")
+        n = B.swarm_tree_attn_workspace_bytes(self.shape, T)
+        if getattr(self, "_tree_ws", None) is None or self._tree_ws.numel() < n:
+            self._tree_ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self._allocated_for(stream, out, lse, self._tree_ws)
+        tree = B.make_tree(q=q, k=k, v=v, n_draft=n_draft, mask=mask)
+        sel, n_sel = (self.o.sel, self.o.n_sel) if selected else (None, None)
+        B.swarm_tree_attn(self.ctx, self.inputs, tree, sel, n_sel, self._tree_ws, out, lse, stream)
+        return out, lse
+
+    def append(self, k, v, n_new, path=None, stream=None) -> None:
+        """swarm_append_tokens into the session's pool: the tokens (k / v [B, T, Hkv, d], all or the accepted ``path``), the
+        summaries of the pages they reach and the workload's context lengths, all in place."""
+        cfg = self.cfg
+        if tuple(k.shape) != (cfg.batch, k.shape[1], cfg.n_kv_heads, cfg.head_dim):
+            raise ValueError(f"k must have shape {(cfg.batch, 'T', cfg.n_kv_heads, cfg.head_dim)}, not {tuple(k.shape)}")
+        tokens = B.make_new_tokens(k=k, v=v, n_new=n_new, path=path)
+        B.swarm_append_tokens(self.ctx, self.inputs, tokens, self.w.kv_pool, self.ksum, self.w.ctx_len, stream)
+
+    def compact(self, parent, reserve=None, keep=None, stream=None) -> None:
+        """swarm_plan_pages and swarm_move_pages inside the session's pool: new request j continues old request parent[j]
+        (strictly ascending over the requests that have one; -1: freed) with the pages that ``keep`` holds and reserve[j] spare
+        ones.  Moves K/V, summaries and page2cluster and writes the workload's page_base and ctx_len.  A plan that is refused
+        leaves everything as it was and shows in status()."""
+        dev, n_pool = self.device, self.w.n_pool_pages
+        if getattr(self, "_pages", None) is None:
+            i32 = dict(dtype=torch.int32, device=dev)
+            self._pages = dict(src=torch.empty(n_pool, **i32), dst=torch.empty(n_pool, **i32), n_moves=torch.empty(1, **i32),
+                               base=torch.empty_like(self.w.page_base), len=torch.empty_like(self.w.ctx_len),
+                               ws=torch.empty(B.swarm_move_pages_workspace_bytes(self.shape), dtype=torch.uint8, device=dev))
+        t = self._pages
+        if keep is not None and keep.numel() < n_pool:
+            raise ValueError("keep must have an entry for every page of the pool")
+        plan = B.make_page_plan(page_base=self.w.page_base, ctx_len=self.w.ctx_len, parent=parent, reserve=reserve, keep=keep,
+                                new_page_base=t["base"], new_ctx_len=t["len"], src=t["src"], dst=t["dst"], n_moves=t["n_moves"],
+                                in_place=True)
+        p2c = self.w.page2cluster
+        moves = B.make_page_moves(src=t["src"], dst=t["dst"], n_moves=t["n_moves"], from_pool=self.w.kv_pool, to_pool=self.w.kv_pool,
+                                  from_ksum=self.ksum, to_ksum=self.ksum, from_page2cluster=p2c, to_page2cluster=p2c)
+        self._allocated_for(stream, *t.values())
+        B.swarm_plan_pages(self.ctx, plan, stream)
+        B.swarm_move_pages(self.ctx, moves, t["ws"], stream)
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(dev)):
+            self.w.page_base.copy_(t["base"])
+            self.w.ctx_len.copy_(t["len"])
+
     def status(self) -> int:
         return B.swarm_device_status(self.ctx)
 

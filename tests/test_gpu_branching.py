@@ -1,0 +1,438 @@
+"""Decoding with several continuations, as a serving program runs it: drafted trees attended and committed through a Session, beams
+selected, forked and compacted; on streams, in captured graphs, in pools beyond 32-bit offsets; and what is refused."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_17803_b200 import binding as B
+from paper_2603_17803_b200 import workloads as W
+from paper_2603_17803_b200.session import Session
+from test_gpu_cache_pages import Layout, close, dev, handle, same
+from test_gpu_tree import Case
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def small(**kw):
+    return W.scaled(W.CONFIGS["c2_128k"], **{**dict(batch=3, ctx_len=16 * 180 + 7, top_k=24, n_topics=8), **kw})
+
+
+def rows_of(w, b, lo, hi):
+    """K and V rows [tokens][Hkv][d] of tokens lo..hi-1 of request b."""
+    S = w.cfg.page_size
+    base = int(w.page_base[b])
+    pos = torch.arange(lo, hi, device=w.kv_pool.device)
+    kv = w.kv_pool[base + pos // S, :, :, pos % S]              # [n][Hkv][2][d]
+    return kv[:, :, 0], kv[:, :, 1]
+
+
+def test_drafted_rounds_rebuild_the_context_they_were_cut_from():
+    """A context is cut short, then grown back by rounds of drafting: a tree whose accepted path is what was cut, attended over the
+    selected pages, its path appended; the rest as a prompt.  Pool, summaries, lengths and the next step are then those of the
+    whole context, bit for bit."""
+    cfg = small()
+    whole = W.generate(cfg, seed=5, device=DEV)
+    ref = Session(whole)
+    ref.step()
+    torch.cuda.synchronize()
+    cut = W.generate(cfg, seed=5, device=DEV)
+    lens = cut.ctx_len.tolist()
+    short = [lens[0] - 37, lens[1] - 1, lens[2] - 20]
+    for b, n in enumerate(short):                               # what is cut is gone
+        S, base = cfg.page_size, int(cut.page_base[b])
+        pos = torch.arange(n, lens[b], device=DEV)
+        cut.kv_pool[base + pos // S, :, :, pos % S] = float("nan")
+    cut.ctx_len.copy_(dev(short))
+    s = Session(cut)
+    rng = np.random.default_rng(1)
+    T, path_len = 9, 4
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    for _ in range(12):
+        left = [lens[b] - int(cut.ctx_len[b]) for b in range(3)]
+        if max(left) == 0:
+            break
+        n_acc = [min(x, int(rng.integers(1, path_len + 1))) for x in left]
+        q = torch.randn((3, T, cfg.n_q_heads, 128), generator=gen, device=DEV).to(torch.bfloat16)
+        k, v = (torch.randn((3, T, cfg.n_kv_heads, 128), generator=gen, device=DEV).to(torch.bfloat16) for _ in range(2))
+        path = np.full((3, path_len), -1)
+        sees = np.zeros((3, T, T), dtype=bool)
+        for b in range(3):
+            at = np.sort(rng.permutation(T)[: n_acc[b]])
+            path[b, : n_acc[b]] = at
+            if n_acc[b]:
+                n0 = int(cut.ctx_len[b])
+                k[b, at], v[b, at] = rows_of(whole, b, n0, n0 + n_acc[b])
+            for t in range(T):
+                sees[b, t, t] = True
+                before = [x for x in at if x < t]
+                if t in at and before:
+                    sees[b, t] |= sees[b, before[-1]]
+        bits = (sees.astype(np.uint64) << np.arange(T, dtype=np.uint64)).sum(-1).astype(np.uint32)
+        mask = torch.from_numpy(bits.view(np.int32)[..., None].copy()).to(DEV)
+        nd = dev([T, T - 1, T])
+        s.select()
+        out, lse = s.tree_attn(q, k, v, nd, mask, selected=True)
+        # the attention itself, for one request and a head, against the formula
+        b, h = 0, 5
+        n0, S, kvh = int(cut.ctx_len[b]), cfg.page_size, 5 // cfg.group
+        pages = s.o.sel[b, h, : int(s.o.n_sel[b, h])].long()
+        pos = (pages[:, None] * S + torch.arange(S, device=DEV)).view(-1)
+        pos = pos[pos < n0]
+        kv = cut.kv_pool[int(cut.page_base[b]) + pos // S, kvh, :, pos % S].double()
+        K, V = torch.cat([kv[:, 0], k[b, :, kvh].double()]), torch.cat([kv[:, 1], v[b, :, kvh].double()])
+        x = q[b, :, h].double() @ K.T / math.sqrt(128)
+        x[:, len(pos):][~torch.from_numpy(sees[b]).to(DEV)] = -math.inf
+        w = torch.softmax(x, -1)
+        want, W_ = w @ V, w @ V.abs()
+        # half a step of bf16 for the weights and for the result (2^-8 each), and 2^-9 for all that is done in fp32
+        tol = 2.0 ** -8 * (W_ + want.abs()) * 1.01 + 2.0 ** -9 * W_
+        assert bool(((out[b, :, h].double() - want).abs() <= tol).all())
+        assert (lse[b, :, h].double() - torch.logsumexp(x, -1)).abs().max().item() < 1e-3
+        s.append(k, v, dev(n_acc), dev(path))
+    left = [lens[b] - int(cut.ctx_len[b]) for b in range(3)]
+    if max(left):                                               # the rest as a prompt
+        n = max(left)
+        k, v = (torch.zeros((3, n, cfg.n_kv_heads, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        for b, m in enumerate(left):
+            if m:
+                k[b, :m], v[b, :m] = rows_of(whole, b, lens[b] - m, lens[b])
+        s.append(k, v, dev(left))
+    assert cut.ctx_len.tolist() == lens
+    for b in range(3):
+        for a, c in zip(rows_of(whole, b, 0, lens[b]), rows_of(cut, b, 0, lens[b])):
+            assert same(a.contiguous(), c.contiguous())
+    assert torch.equal(s.ksum.float(), ref.ksum.float())
+    s.step()
+    torch.cuda.synchronize()
+    for f in ("sel", "n_sel", "out", "lse", "queue_load"):
+        assert torch.equal(getattr(s.o, f), getattr(ref.o, f)), f
+    assert s.status() == 0 and ref.status() == 0
+    s.close()
+    ref.close()
+
+
+def test_single_token_tree_is_the_step_over_all_pages():
+    """With as many places as pages every page is selected: the step's attention and a tree of one token that sees only the
+    context are the same sum, up to the rounding of the weights and of the result to bf16 (2^-8 each)."""
+    cfg = small(ctx_len=16 * 40 + 3, top_k=64)
+    w = W.generate(cfg, seed=9, device=DEV)
+    s = Session(w)
+    s.step()
+    zero = torch.zeros((3, 1, cfg.n_kv_heads, 128), dtype=torch.bfloat16, device=DEV)
+    mask = torch.zeros((3, 1, 1), dtype=torch.int32, device=DEV)
+    for selected in (False, True):
+        out, lse = s.tree_attn(w.q[:, None], zero, zero, dev([1, 1, 1]), mask, selected=selected)
+        torch.cuda.synchronize()
+        vmax = w.kv_pool[:, :, 1].abs().max().item()
+        assert (out[:, 0].float() - s.o.out).abs().max().item() <= 2.0 ** -8 * 2 * vmax
+        assert (lse[:, 0] - s.o.lse).abs().max().item() <= 1e-4
+    s.close()
+
+
+def test_beams_are_selected_forked_and_attended():
+    """Two prompts of three beams: the selection's parents go into the plan, the moves into a second pool; every beam then attends
+    exactly what its parent attended."""
+    batch, beams, hkv, S = 6, 3, 2, 16
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    lens, pages = [100] * 3 + [333] * 3, [8] * 3 + [22] * 3
+    base = np.concatenate([[0], np.cumsum(pages)])
+    n_pool = int(base[-1]) + 4
+    pool = torch.randn((n_pool, hkv, 2, S, 128), generator=gen, device=DEV).to(torch.bfloat16)
+    other = torch.full_like(pool, float("nan"))
+    shape, ctx, ws = handle(batch, hkv, S, n_pool, max(pages))
+    logits = torch.randn((2, beams, 777), generator=gen, device=DEV) * 3
+    score = torch.tensor([[-1.0, -0.5, -2.0], [-0.1, -9.0, -0.2]], device=DEV)
+    new, parent, token = torch.empty((2, beams), device=DEV), *(torch.empty((2, beams), dtype=torch.int32, device=DEV) for _ in range(2))
+    bws = torch.empty(B.swarm_beam_select_workspace_bytes(2, beams, 777, beams), dtype=torch.uint8, device=DEV)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    src, dst, n_moves, new_len = torch.empty(n_pool, **i32), torch.empty(n_pool, **i32), torch.empty(1, **i32), torch.empty(batch, **i32)
+    page_base, new_base, ctx_len = dev(base, torch.int64), torch.empty(batch + 1, dtype=torch.int64, device=DEV), dev(lens)
+    mws = torch.empty(B.swarm_move_pages_workspace_bytes(shape), dtype=torch.uint8, device=DEV)
+    B.swarm_beam_select(logits, score, bws, new, parent, token)
+    plan = B.make_page_plan(page_base=page_base, ctx_len=ctx_len, parent=parent.view(-1), new_page_base=new_base, new_ctx_len=new_len,
+                            src=src, dst=dst, n_moves=n_moves)
+    B.swarm_plan_pages(ctx, plan)
+    B.swarm_move_pages(ctx, B.make_page_moves(src=src, dst=dst, n_moves=n_moves, from_pool=pool, to_pool=other), mws)
+    q = torch.randn((batch, 1, hkv, 128), generator=gen, device=DEV).to(torch.bfloat16)
+    kv = torch.randn((2, batch, 1, hkv, 128), generator=gen, device=DEV).to(torch.bfloat16)
+    tws = torch.empty(B.swarm_tree_attn_workspace_bytes(shape, 1), dtype=torch.uint8, device=DEV)
+    outs = []
+    up = parent.view(-1).long()
+    assert sorted(set((up // 3).tolist())) == [0, 1] and up[:3].max() < 3 and up[3:].min() >= 3
+    for p, pb, cl, qq, kk, vv in ((pool, page_base, ctx_len, q[up], kv[0][up], kv[1][up]), (other, new_base, new_len, q[up], kv[0][up], kv[1][up])):
+        # the first run attends the parents where they were: request j's pages are those of parent j
+        if p is pool:
+            starts = torch.stack([page_base[up], page_base[up + 1]], 1)
+            out = torch.empty((batch, 1, hkv, 128), dtype=torch.bfloat16, device=DEV)
+            lse = torch.empty((batch, 1, hkv), device=DEV)
+            for j in range(batch):                              # one request at a time, in its parent's place
+                one_shape, one, one_ws = handle(1, hkv, S, n_pool, max(pages))
+                held = [x[j: j + 1].contiguous() for x in (qq, kk, vv)] + [dev([1])]
+                t1 = B.make_tree(q=held[0], k=held[1], v=held[2], n_draft=held[3])
+                o1, l1 = torch.empty((1, 1, hkv, 128), dtype=torch.bfloat16, device=DEV), torch.empty((1, 1, hkv), device=DEV)
+                pb1, cl1 = starts[j].contiguous(), cl[up[j]: up[j] + 1].clone()
+                B.swarm_tree_attn(one, B.make_inputs(kv_pool=p, page_base=pb1, ctx_len=cl1), t1, None, None, tws, o1, l1)
+                torch.cuda.synchronize()
+                out[j], lse[j] = o1[0], l1[0]
+                close(one)
+        else:
+            out = torch.empty((batch, 1, hkv, 128), dtype=torch.bfloat16, device=DEV)
+            lse = torch.empty((batch, 1, hkv), device=DEV)
+            held = [x.contiguous() for x in (qq, kk, vv)] + [dev([1] * batch)]
+            tree = B.make_tree(q=held[0], k=held[1], v=held[2], n_draft=held[3])
+            B.swarm_tree_attn(ctx, B.make_inputs(kv_pool=p, page_base=pb, ctx_len=cl), tree, None, None, tws, out, lse)
+        outs.append((out.float(), lse))
+    torch.cuda.synchronize()
+    # the same tokens, cut differently over the CTAs: fp32 sums in another order, then a rounding to bf16 (2^-8 of the value)
+    assert bool(((outs[0][0] - outs[1][0]).abs() <= 2.0 ** -7 * outs[0][0].abs() + 1e-3).all())
+    assert (outs[0][1] - outs[1][1]).abs().max().item() < 1e-4
+    assert B.swarm_device_status(ctx) == 0
+    close(ctx)
+
+
+def test_compaction_keeps_the_step():
+    """A request is freed and the others moved together: their selection and attention stay what they were."""
+    cfg = small(batch=4)
+    w = W.generate(cfg, seed=6, device=DEV)
+    s = Session(w)
+    s.step()
+    torch.cuda.synchronize()
+    before = [x.clone() for x in (s.o.sel, s.o.out, s.o.lse)]
+    base = w.page_base.tolist()
+    s.compact(dev([-1, 0, 2, 3]), reserve=dev([1, 0, 2, 0]))
+    assert s.status() == 0
+    n = [base[1] - base[0], base[3] - base[2], base[4] - base[3]]
+    assert w.page_base.tolist() == [0, 1, 1 + n[0], 3 + n[0] + n[1], 3 + sum(n)] and w.ctx_len.tolist()[0] == 0
+    w.ctx_len[0] = 1                                            # (a step wants a token in every request)
+    w.kv_pool[0] = 0
+    s.ksum[0] = 0
+    s.set_query(w.q[[0, 0, 2, 3]].contiguous())
+    s.select()
+    s.sparse_attn_paged()
+    torch.cuda.synchronize()
+    for got, was in zip((s.o.sel, s.o.out, s.o.lse), before):
+        for new, old in ((1, 0), (2, 2), (3, 3)):
+            assert torch.equal(got[new], was[old])
+    s.compact(dev([3, 2, 1, 0]))                                # refused: not in order
+    assert s.status() == B.DEV_BAD_PAGE and w.page_base.tolist()[-1] == 3 + sum(n)
+    s.close()
+
+
+def test_a_captured_round_replays():
+    """Attention, commit, plan and moves, and a beam selection in one CUDA graph, replayed: each replay equals the calls by themselves."""
+    c = Case(lens=[70, 300], T=6, n_draft=[6, 4], hq=8, hkv=2, S=16, seed=4, spare=3)
+    n_pool = c.pool.shape[0]
+    i32 = dict(dtype=torch.int32, device=DEV)
+    new_len = torch.zeros(4, **i32)
+    pool = torch.where(torch.isnan(c.pool), torch.zeros_like(c.pool), c.pool)
+    ksum = torch.zeros((n_pool, 2, 2, 128), dtype=torch.bfloat16, device=DEV)
+    B.swarm_build_summaries(c.ctx, B.make_inputs(kv_pool=pool, page_base=c.page_base, ctx_len=c.ctx_len), ksum)
+    n_new, path = dev([2, 3]), dev([[0, 4, -1], [1, 2, 3]])
+    tokens = B.make_new_tokens(k=c.k, v=c.v, n_new=n_new, path=path)
+    t = dict(src=torch.zeros(n_pool, **i32), dst=torch.zeros(n_pool, **i32), n_moves=torch.zeros(4, **i32))
+    nb, nl = torch.zeros(3, dtype=torch.int64, device=DEV), torch.zeros(4, **i32)
+    parent, reserve = dev([1, 0]), dev([1, 1])
+    plan = B.make_page_plan(page_base=c.page_base, ctx_len=new_len[:2], parent=parent, reserve=reserve, new_page_base=nb,
+                            new_ctx_len=nl[:2], src=t["src"], dst=t["dst"], n_moves=t["n_moves"])
+    second = torch.zeros_like(pool)
+    moves = B.make_page_moves(src=t["src"], dst=t["dst"], n_moves=t["n_moves"], from_pool=pool, to_pool=second)
+    mws = torch.empty(B.swarm_move_pages_workspace_bytes(c.shape), dtype=torch.uint8, device=DEV)
+    logits, score = torch.randn((1, 2, 900), device=DEV), torch.zeros((1, 2), device=DEV)
+    bws = torch.empty(B.swarm_beam_select_workspace_bytes(1, 2, 900, 4), dtype=torch.uint8, device=DEV)
+    beam = torch.empty((1, 4), device=DEV), torch.empty((1, 4), **i32), torch.empty((1, 4), **i32)
+    inputs = B.make_inputs(kv_pool=pool, page_base=c.page_base, ctx_len=c.ctx_len)
+
+    def once():
+        B.swarm_tree_attn(c.ctx, inputs, c.tree, None, None, c.ws, c.out, c.lse)
+        B.swarm_append_tokens(c.ctx, inputs, tokens, pool, ksum, new_len)
+        B.swarm_plan_pages(c.ctx, plan)
+        B.swarm_move_pages(c.ctx, moves, mws)
+        B.swarm_beam_select(logits, score, bws, *beam)
+
+    results = (c.out, c.lse, pool, ksum, new_len, nb, nl, second, *beam)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        once()
+        st.synchronize()
+        c.check()
+        want = [x.clone() for x in results]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            once()
+            once()
+        for x in (c.out, c.lse):
+            x.fill_(7.0)
+        for x in (new_len, nb, nl, second, *beam):
+            x.zero_()
+        for _ in range(3):
+            g.replay()
+        st.synchronize()
+    for x, y in zip(results, want):
+        assert same(x, y)
+    assert B.swarm_device_status(c.ctx) == 0
+    c.close()
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    """Two contexts, two streams, no order between them."""
+    a = Case(lens=[900, 40, 0, 333], T=20, n_draft=[20, 3, 20, 11], hq=8, hkv=2, S=16, seed=11)
+    b = Case(lens=[2000], T=70, n_draft=[66], hq=8, hkv=2, S=32, seed=12)
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        a.run(sa)
+        b.run(sb)
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
+    a.close()
+    b.close()
+
+
+def test_calls_back_to_back_on_one_workspace():
+    """Each call's kernels follow the last one's on the stream: nothing of one is left in the next."""
+    c = Case(lens=[500, 77], T=12, n_draft=[12, 5], hq=16, hkv=2, S=16, seed=21)
+    for _ in range(30):
+        c.run()
+    c.check()
+    c.nd.copy_(dev([3, 0]))
+    c.n_draft = [3, 0]
+    c.out.fill_(7.0)
+    c.lse.fill_(7.0)
+    c.run()
+    c.check()
+    c.close()
+
+
+def test_pools_beyond_32_bit_offsets():
+    """A request at the end of a pool of 12 GB: attended, appended to, moved."""
+    hkv, S, n_pool = 8, 16, 196608                              # 64 KB a page
+    pool = torch.empty((n_pool, hkv, 2, S, 128), dtype=torch.bfloat16, device=DEV)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    first, n_pages, length = n_pool - 13, 11, 150
+    pool[first:] = torch.randn((13, hkv, 2, S, 128), generator=gen, device=DEV).to(torch.bfloat16)
+    shape, ctx, ws = handle(1, hkv, S, n_pool, n_pages)
+    page_base, ctx_len = dev([first, first + n_pages], torch.int64), dev([length])
+    inputs = B.make_inputs(kv_pool=pool, page_base=page_base, ctx_len=ctx_len)
+    q = torch.randn((1, 2, hkv, 128), generator=gen, device=DEV).to(torch.bfloat16)
+    k, v = (torch.randn((1, 2, hkv, 128), generator=gen, device=DEV).to(torch.bfloat16) for _ in range(2))
+    out, lse = torch.empty_like(q), torch.empty((1, 2, hkv), device=DEV)
+    tws = torch.empty(B.swarm_tree_attn_workspace_bytes(shape, 2), dtype=torch.uint8, device=DEV)
+    two = dev([2])
+    B.swarm_tree_attn(ctx, inputs, B.make_tree(q=q, k=k, v=v, n_draft=two), None, None, tws, out, lse)
+    for h in range(hkv):
+        kv = pool[first: first + n_pages, h].transpose(1, 2).reshape(-1, 2, 128)[:length].double()
+        K, V = torch.cat([kv[:, 0], k[0, :, h].double()]), torch.cat([kv[:, 1], v[0, :, h].double()])
+        x = q[0, :, h].double() @ K.T / math.sqrt(128)
+        x[0, -1] = -math.inf
+        w = torch.softmax(x, -1)
+        tol = 2.0 ** -8 * (w @ V.abs() + (w @ V).abs()) * 1.01 + 2.0 ** -9 * (w @ V.abs())
+        assert bool(((out[0, :, h].double() - w @ V).abs() <= tol).all())
+    new_len = torch.zeros(1, dtype=torch.int32, device=DEV)
+    want = pool[first:].clone()
+    for i in range(2):
+        p, slot = (length + i) // S, (length + i) % S
+        want[p, :, 0, slot], want[p, :, 1, slot] = k[0, i], v[0, i]
+    B.swarm_append_tokens(ctx, inputs, B.make_new_tokens(k=k, v=v, n_new=two), pool, None, new_len)
+    torch.cuda.synchronize()
+    assert same(pool[first:], want) and new_len.tolist() == [length + 2]
+    mws = torch.empty(B.swarm_move_pages_workspace_bytes(shape), dtype=torch.uint8, device=DEV)
+    src, dst = dev([first, first + 1]), dev([0, n_pool - 1])
+    B.swarm_move_pages(ctx, B.make_page_moves(src=src, dst=dst, n_moves=two, from_pool=pool, to_pool=pool), mws)
+    torch.cuda.synchronize()
+    assert same(pool[0], want[0]) and same(pool[-1], want[1])
+    assert B.swarm_device_status(ctx) == 0
+    close(ctx)
+
+
+@pytest.mark.parametrize("hq,hkv,T", [(128, 1, 3), (100, 1, 2), (65, 1, 4), (33, 33, 5)])
+def test_wide_head_groups(hq, hkv, T):
+    c = Case(lens=[200, 31], T=T, n_draft=[T, 1], hq=hq, hkv=hkv, S=16, seed=hq)
+    c.run()
+    c.check()
+    c.close()
+
+
+def test_lengths_that_do_not_fit_are_reported_and_left_alone():
+    c = Case(lens=[100, 50, 30], T=4, n_draft=[4, 4, 4], hq=8, hkv=2, S=16, seed=2, spare=0)
+    c.ctx_len.copy_(dev([100, 50 + 16 * 3, -2]))                # requests 1 and 2 do not fit
+    c.nd.copy_(dev([9, 4, 4]))                                  # more than there are: clamped
+    c.run()
+    torch.cuda.synchronize()
+    assert B.swarm_device_status(c.ctx) == B.DEV_BAD_LENGTH
+    assert bool((c.out[1:] == 7.0).all()) and bool((c.lse[1:] == 7.0).all())
+    c.n_draft, c.batch = [4], 1
+    c.check()
+    c.ctx_len.copy_(dev([100, 50, 30]))
+    c.nd.copy_(dev([-1, 4, 4]))
+    c.out.fill_(7.0)
+    c.lse.fill_(7.0)
+    c.run()
+    assert B.swarm_device_status(c.ctx) == B.DEV_BAD_LENGTH
+    c.n_draft, c.batch = [0, 4, 4], 3
+    c.check()
+    c.close()
+
+
+def test_selections_with_bad_and_repeated_pages():
+    c = Case(lens=[300, 100], T=3, n_draft=[3, 3], hq=4, hkv=2, S=16, seed=3, top_k=8)
+    c.sel[0, 1, :3] = dev([5, 5, 5])                            # the same page again: counts once
+    good = c.sel.clone()
+    c.run()
+    c.check()
+    assert B.swarm_device_status(c.ctx) == 0
+    c.sel[0, 0, 2] = 19                                         # behind the request's last page
+    c.sel[1, 3, 0] = -4
+    c.out.fill_(7.0)
+    c.lse.fill_(7.0)
+    c.run()
+    assert B.swarm_device_status(c.ctx) == B.DEV_BAD_PAGE
+    c.sel = good                                                # what is left: the list without those places
+    sel, n = c.sel.clone(), c.n_sel.clone()
+    keep = [x for i, x in enumerate(sel[0, 0, : int(n[0, 0])].tolist()) if i != 2]
+    c.sel[0, 0, : len(keep)] = dev(keep)
+    c.n_sel[0, 0] = len(keep)
+    keep = sel[1, 3, 1: int(n[1, 3])].tolist()
+    c.sel[1, 3, : len(keep)] = dev(keep)
+    c.n_sel[1, 3] = len(keep)
+    c.check()
+    c.close()
+
+
+def test_arguments_are_checked():
+    c = Case(lens=[20], T=2, n_draft=[2], hq=4, hkv=2, S=16, seed=1)
+    with pytest.raises(ValueError):
+        B.make_tree(q=c.q, k=c.k, v=c.v.float(), n_draft=c.nd)
+    with pytest.raises(ValueError):
+        B.make_tree(q=c.q, k=c.k, v=c.v, n_draft=c.nd, mask=torch.zeros((1, 2, 2), dtype=torch.int32, device=DEV))
+    with pytest.raises(ValueError):
+        B.make_tree(q=c.q.transpose(1, 2), k=c.k, v=c.v, n_draft=c.nd)
+    with pytest.raises(ValueError):
+        B.swarm_tree_attn(c.ctx, c.inputs, c.tree, None, None, c.ws, c.out.float(), c.lse)
+    for kw, code in ((dict(ws=c.ws[:256]), B.ERR_WORKSPACE_TOO_SMALL), (dict(sel=dev([0])), B.ERR_INVALID_ARG),
+                     (dict(ws=c.ws_all[16:]), B.ERR_INVALID_ARG)):
+        with pytest.raises(B.SwarmError) as e:
+            B.swarm_tree_attn(c.ctx, c.inputs, c.tree, kw.get("sel"), None, kw.get("ws", c.ws), c.out, c.lse)
+        assert e.value.code == code, kw
+    bad = B.make_inputs(page_base=c.page_base, ctx_len=c.ctx_len)
+    with pytest.raises(B.SwarmError) as e:
+        B.swarm_tree_attn(c.ctx, bad, c.tree, None, None, c.ws, c.out, c.lse)
+    assert e.value.code == B.ERR_INVALID_ARG
+    tokens = B.make_new_tokens(k=c.k, v=c.v, n_new=c.nd)
+    tokens.max_path = 3                                         # a path that is not there
+    with pytest.raises(B.SwarmError) as e:
+        B.swarm_append_tokens(c.ctx, c.inputs, tokens, c.pool, None, c.nd)
+    assert e.value.code == B.ERR_INVALID_ARG
+    lay = Layout([16], [1], 8)
+    with pytest.raises(B.SwarmError) as e:                      # the new tables may not be the old ones
+        lay.plan([0])
+        p = B.make_page_plan(page_base=lay.page_base, ctx_len=lay.ctx_len, parent=lay.held[0], new_page_base=lay.page_base,
+                             new_ctx_len=lay.new_len, src=lay.src, dst=lay.dst, n_moves=lay.n)
+        B.swarm_plan_pages(lay.ctx, p)
+    assert e.value.code == B.ERR_INVALID_ARG
+    close(lay.ctx)
+    c.close()
