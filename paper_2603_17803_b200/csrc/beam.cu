@@ -150,7 +150,8 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   constexpr int kVec = 16 / (int)sizeof(T), kVecs = kPer / kVec, kChunk = kBeamThreads * kPer;
   constexpr int kMany = 64;                                   // threads with a candidate that are gathered as they are
   __shared__ key_t s_max[128];
-  __shared__ key_t s_cand[kMaxBeamKeep + 128 * kPer];
+  constexpr int kRoom = kMaxBeamKeep + 128 * kPer;
+  __shared__ key_t s_cand[kRoom];
   __shared__ key_t s_top[kMaxBeamKeep];
   __shared__ float2 s_red[kBeamThreads / 32];
   __shared__ key_t s_bound;
@@ -169,7 +170,8 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   const int begin = stretch * span * kChunk, stop = min(V, begin + span * kChunk);
   // chunks of this stretch whose vectors (with the line behind, where they are put together) lie inside the row and the tensor
   const int n_whole = max(0, (int)min((long long)(stop - begin), (long long)(end - 32 - first) / (int)sizeof(T) - begin) / kChunk);
-  const char* next = first + ((long long)begin + tid * kVec) * (int)sizeof(T) - shift;
+  const char* const start = first + ((long long)begin + tid * kVec) * (int)sizeof(T) - shift;
+  const char* next = start;
   uint4 raw[kVecs];
   auto fetch = [&] {
     if (shift == 0) {
@@ -215,7 +217,13 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
       floor_ = key_value(s_top[keep - 1]);
     }
   };
+  // Behind the first chunk candidates are rare, and no barrier is spent on them: a thread appends what lies above the floor it knows,
+  // and the gathered ones are ranked after 1, 2, 4, 8, 16, 24 ... chunks, each time about as many again as are kept.
+  // Where more come than there is room for (logits that rise along the row), the stretch is done again with a look at every chunk.
+  bool over = false;
+  for (bool careful = false;; careful = true) {
   if (n_whole > 0) fetch();
+  bool more = false;                                          // this thread has appended since the last ranking
   for (int at0 = begin, chunk = 0; at0 < stop; at0 += kChunk, ++chunk) {
     float x[kPer];
     if (chunk < n_whole) {
@@ -248,7 +256,30 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
       sum += sum_exp(x, ref);
     }
 
-    // Candidates: logits above the floor.  They are ranked, and the floor raised, when enough have come together.
+    // Candidates: logits above the floor.
+    auto token = [&](int e) { return (uint32_t)(at0 + ((e / kVec) * kBeamThreads + tid) * kVec + e % kVec); };
+    if (!careful && chunk > 0) {
+      if (__any_sync(0xFFFFFFFFu, mine > floor_)) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+          if (x[e] > floor_) {
+            const int at = atomicAdd(&s_count, 1);
+            if (at < kRoom) s_cand[at] = make_key(x[e], token(e));
+            else over = true;
+            more = true;
+          }
+        }
+      }
+      if ((chunk & (chunk + 1)) == 0 || (chunk & 7) == 7) {
+        if (__syncthreads_or(more)) {
+          if (__syncthreads_or(over)) break;
+          rank();
+          __syncthreads();
+          more = false;
+        }
+      }
+      continue;
+    }
     const int hits = __syncthreads_count(mine > floor_);
     if (hits == 0) continue;
     const int held = s_count;
@@ -257,7 +288,6 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
       rank();
       __syncthreads();
     }
-    auto token = [&](int e) { return (uint32_t)(at0 + ((e / kVec) * kBeamThreads + tid) * kVec + e % kVec); };
     key_t bound = 0;
     float bound_value = -INFINITY;
     if (hits > kMany) {
@@ -296,8 +326,20 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
         }
       }
     }
+    if (!careful) {                                           // (the first chunk: a floor for the others)
+      __syncthreads();
+      rank();
+      __syncthreads();
+    }
   }
-  __syncthreads();
+  if (!__syncthreads_or(over)) break;
+  // once more, from the start
+  over = false;
+  if (tid == 0) s_count = 0;
+  top = floor_ = -INFINITY;
+  sum = 0.f;
+  next = start;
+  }
   if (s_count > keep) rank();
   __syncthreads();
   // the threads' sums

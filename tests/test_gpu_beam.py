@@ -136,6 +136,20 @@ def test_lowest_finite_logits_as_a_mask():
     assert torch.equal(new, torch.tensor([[-0.5, -1.0], [-0.5, -1.0]], device=DEV))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("order", ["rising", "falling", "late", "one_late"])
+def test_logits_in_order(order, dtype):
+    """Rows whose large logits come last (every chunk brings more candidates than there is room for), first, or behind tens of
+    thousands of masked ones; long enough that a CTA goes through many chunks."""
+    gen = torch.Generator(device=DEV).manual_seed(17)
+    logits = torch.randn((90, 2, 70001), generator=gen, device=DEV).sort(-1, descending=order == "falling").values.to(dtype)
+    if order in ("late", "one_late"):
+        logits[..., : 60000] = -math.inf
+    if order == "one_late":
+        logits[..., : -1] = -math.inf
+    check(logits, -torch.rand((90, 2), generator=gen, device=DEV), 24)
+
+
 def test_padded_rows():
     gen = torch.Generator(device=DEV).manual_seed(3)
     whole = torch.full((2, 3, 1100), math.inf, device=DEV)
