@@ -487,6 +487,8 @@ int32_t swarm_tree_attn(swarm_ctx* ctx, const swarm_inputs* inputs, const swarm_
  * the accepted path of a drafted tree (new->path; a token may be named twice) and for prompts.
  * A request whose new length does not fit the pages it owns (or with n_new out of range) sets SWARM_DEV_BAD_LENGTH and
  * is left as it was.  A path entry outside 0..T-1 sets SWARM_DEV_BAD_TOKEN; its rows are written as zeros.
+ * page2cluster entries of pages that are written to for the first time are the caller's.  With a tail stream, swarm_tail_join
+ * comes first; with the index prefetch on, at least one operation between this call and the step.
  * Reads inputs->page_base, ctx_len.  kv_pool as in swarm_inputs, ksum bf16 [n_pool_pages][Hkv][2][d] or NULL. */
 int32_t swarm_append_tokens(swarm_ctx* ctx, const swarm_inputs* inputs, const swarm_new_tokens* tokens, void* kv_pool,
                             void* ksum, int32_t* ctx_len_out, void* stream);
@@ -512,7 +514,10 @@ int32_t swarm_plan_pages(swarm_ctx* ctx, const swarm_page_plan* plan, void* stre
  * one reads: true for every plan of swarm_plan_pages, and for copies to pages that are not sources.  A pair that breaks this,
  * a second pair with the same dst, and ids outside the pool set SWARM_DEV_BAD_PAGE and are skipped.
  * workspace: swarm_move_pages_workspace_bytes(shape) bytes of device memory (256-byte aligned, contents irrelevant), used by
- * one call at a time; < 0: minus an error code. */
+ * one call at a time; < 0: minus an error code.  SWARM_ERR_UNSUPPORTED: n_pool_pages or max_moves >= 2^30, or more than about 2^31
+ * blocks of 32 KB in max_moves pages.
+ * page2cluster holds ids local to a request and is moved as it is: where requests change places, cluster_base and the
+ * tables it points into are the caller's to permute.  With a tail stream, swarm_tail_join comes before moves inside the pool. */
 int64_t swarm_move_pages_workspace_bytes(const swarm_shape* shape);
 int32_t swarm_move_pages(swarm_ctx* ctx, const swarm_page_moves* moves, void* workspace, int64_t workspace_bytes, void* stream);
 
@@ -525,7 +530,7 @@ int32_t swarm_move_pages(swarm_ctx* ctx, const swarm_page_moves* moves, void* wo
  * Logits must be below +inf.  logits: SWARM_DTYPE_*, row (b, k) starts (b * n_beams + k) * row_stride elements behind the
  * first (row_stride >= vocab).  score f32 [batch][n_beams]; outputs [batch][n_keep]; 1 <= n_keep <= 64.
  * workspace: swarm_beam_select_workspace_bytes bytes of device memory (contents irrelevant), used by one call at a time;
- * < 0: minus an error code.  SWARM_ERR_UNSUPPORTED: n_beams * vocab >= 2^31, or too many candidates
+ * < 0: minus an error code.  SWARM_ERR_UNSUPPORTED: vocab >= 2^30, n_beams * vocab >= 2^31, or too many candidates
  * (n_beams * vocab / 8192 * n_keep^2 beyond about 6 million). */
 int64_t swarm_beam_select_workspace_bytes(int32_t batch, int32_t n_beams, int32_t vocab, int32_t n_keep);
 int32_t swarm_beam_select(const void* logits, int32_t dtype, int64_t row_stride, const float* score, int32_t batch,

@@ -593,8 +593,8 @@ def swarm_beam_select(logits: torch.Tensor, score: torch.Tensor, workspace: torc
     if logits.dtype not in _LOGIT_TYPES or logits.dim() != 3:
         raise ValueError("logits must be a float32, bfloat16 or float16 tensor of three dimensions")
     batch, beams, vocab = logits.shape
-    if not logits.is_cuda:
-        raise ValueError("logits must be a CUDA tensor")
+    if not logits.is_cuda or logits.get_device() != torch.cuda.current_device():
+        raise ValueError("logits must be a CUDA tensor on the current device")
     pitch = logits.stride(1) if beams > 1 else logits.stride(0) if batch > 1 else vocab
     if logits.stride(2) != 1 and vocab > 1 or pitch < vocab or (batch > 1 and logits.stride(0) != beams * pitch):
         raise ValueError("logits must have contiguous rows at one distance")

@@ -966,7 +966,7 @@ int32_t swarm_move_pages(swarm_ctx* ctx, const swarm_page_moves* m, void* worksp
       workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u))
     return SWARM_ERR_INVALID_ARG;
   const Geometry& g = ctx->geo;
-  if (!pages_supported(g) || m->max_moves >= (1 << 30)) return SWARM_ERR_UNSUPPORTED;
+  if (!pages_supported(g) || !moves_supported(g, m->max_moves)) return SWARM_ERR_UNSUPPORTED;
   if (workspace_bytes < move_pages_workspace_bytes(g)) return SWARM_ERR_WORKSPACE_TOO_SMALL;
   // every table goes to itself, or to memory that does not overlap it
   const bool in_place = m->from_pool == m->to_pool;

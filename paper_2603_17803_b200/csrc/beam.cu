@@ -515,6 +515,7 @@ int most_stretches(long long rows, int vocab) {
 }  // namespace
 
 bool beam_supported(int batch, int n_beams, int vocab, int n_keep) {
+  if (vocab >= (1 << 30)) return false;                       // (tokens are counted in 32 bits up to the end of a row's last stretch)
   const long long rows = (long long)batch * n_beams;
   const int parts = most_stretches(rows, vocab);
   return (long long)n_beams * vocab < (1LL << 31) && rows * parts < (1LL << 31) && (long long)n_beams * parts * n_keep < (1LL << 30) &&

@@ -332,6 +332,13 @@ cudaError_t configure_pages() { return cudaFuncSetAttribute(move_kernel, cudaFun
 
 bool pages_supported(const Geometry& geo) { return geo.n_pool_pages < (1LL << 30); }
 
+// The queue of items (both directions of every pair) is counted in 32 bits, and every CTA counts once more at its end.
+bool moves_supported(const Geometry& geo, int max_moves) {
+  const long long page = (long long)geo.Hkv * 2 * geo.S * kHeadDim * 2, sums = (long long)geo.Hkv * 2 * kHeadDim * 2;
+  const long long items = (page + kChunk - 1) / kChunk + (sums + kChunk - 1) / kChunk;
+  return max_moves < (1 << 30) && 2 * items * max_moves < (1LL << 32) - (1 << 20);
+}
+
 long long move_pages_workspace_bytes(const Geometry& geo) { return 256 + 3 * align256(geo.n_pool_pages * 4); }
 
 cudaError_t launch_plan_pages(const Geometry& geo, const PlanCall& c, uint32_t* status, cudaStream_t st) {

@@ -364,6 +364,7 @@ struct MoveCall {
 };
 cudaError_t configure_pages();
 bool pages_supported(const Geometry& geo);
+bool moves_supported(const Geometry& geo, int max_moves);
 long long move_pages_workspace_bytes(const Geometry& geo);
 cudaError_t launch_plan_pages(const Geometry& geo, const PlanCall& c, uint32_t* status, cudaStream_t st);
 cudaError_t launch_move_pages(const Geometry& geo, const MoveCall& c, void* workspace, uint32_t* status, cudaStream_t st);

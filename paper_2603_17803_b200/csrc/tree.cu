@@ -849,16 +849,18 @@ tree_merge_kernel(const TreeArgs a, int groups, int tiles) {
   const int tile = id % tiles, u = id / tiles;
   const int b = u / a.geo.Hkv, kv = u - b * a.geo.Hkv, g = a.geo.g;
   const int in_tile = group * 32 + lane, t = tile * a.tile_tokens + in_tile / g, h = in_tile % g;
-  // (the caller's tables: nothing between the wait of the kernel in front and here writes them)
-  const int len = a.ctx_len[b];
-  const long long owned = a.page_base[b + 1] - a.page_base[b];
-  const int nd = len < 0 || pages_of(len, a.geo.S) > owned ? 0 : max(0, min(a.n_draft[b], a.T));
+  // (the caller's tables: nothing between the wait of the kernel in front and here writes them; read past L1, since this kernel
+  // has not waited for anything yet)
+  const int len = __ldcg(a.ctx_len + b);
+  const long long owned = __ldcg(a.page_base + b + 1) - __ldcg(a.page_base + b);
+  const int nd = len < 0 || pages_of(len, a.geo.S) > owned ? 0 : max(0, min(__ldcg(a.n_draft + b), a.T));
   pdl_wait();
   const int first = a.unit_first[u], last = a.unit_last[u];  // (not written where nd is 0)
   pdl_launch_dependents();
   if (tile * a.tile_tokens >= nd) return;
   const int c0 = first >> 1, n = last - c0 + 1;
-  if (n == 1) return;                                        // written by the CTA that had the whole unit
+  if (n <= 1) return;                                        // written by the CTA that had the whole unit
+  if (first < 0 || last >= a.chunks) return;                 // (a wait ran out and the unit was not listed: reported)
   const bool here = in_tile < a.tile_tokens * g && t < nd;
   const int rb = tile / kQTiles, r = tile % kQTiles * kTile + min(in_tile, kTile - 1);
   float M = -INFINITY, sum = 0.f;
@@ -1004,7 +1006,7 @@ tree_list_kernel(const TreeArgs a, const int32_t* __restrict__ sel, const int32_
   });
   if (tid == 0) {
     const bool ends = P > 0 && ((s_map[(P - 1) >> 5] >> ((P - 1) & 31)) & 1u);
-    list_tokens[u] = total * S - (ends ? P * S - len : 0);
+    list_tokens[u] = total * S - (ends ? max(0, P * S - len) : 0);
   }
 }
 

@@ -112,3 +112,11 @@ def test_every_plan_that_keeps_the_order_can_be_carried_out_in_place():
         for s, d in pairs:
             want[d] = pool[s]
         assert moved(pairs, pool) == want
+
+
+@pytest.mark.parametrize("vocab", [1 << 30, (1 << 31) - 1])
+def test_rows_that_are_too_long_to_count_are_refused(vocab):
+    with pytest.raises(B.SwarmError) as e:
+        B.swarm_beam_select_workspace_bytes(1, 1, vocab, 1)
+    assert e.value.code == B.ERR_UNSUPPORTED
+    assert B.swarm_beam_select_workspace_bytes(1, 1, (1 << 30) - 1, 1) > 0
