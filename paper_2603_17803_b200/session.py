@@ -54,6 +54,7 @@ class Session:
         B.swarm_set_workspace(self.ctx, self.workspace)
         if scorer != B.SCORER_AUTO:
             B.swarm_set_scorer(self.ctx, scorer)
+        self.index_prefetch = index_prefetch
         if index_prefetch:                       # the workload's index and lengths are written once, before any step
             B.swarm_set_index_prefetch(self.ctx, True)
         self.tail_stream = tail_stream
@@ -200,7 +201,10 @@ class Session:
     def tree_attn(self, q, k, v, n_draft, mask=None, *, selected=False, out=None, lse=None, stream=None):
         """swarm_tree_attn for drafted tokens q [B, T, Hq, d], k / v [B, T, Hkv, d]: over the whole context of every
         request, or, with ``selected``, over the pages of the last select() / step().  Returns (out, lse)."""
-        cfg, T = self.cfg, q.shape[1]
+        cfg = self.cfg
+        if q.dim() != 4:
+            raise ValueError("q must have four dimensions: request, drafted token, head, coordinate")
+        T = q.shape[1]
         for name, t, heads in (("q", q, cfg.n_q_heads), ("k", k, cfg.n_kv_heads), ("v", v, cfg.n_kv_heads)):
             if tuple(t.shape) != (cfg.batch, T, heads, cfg.head_dim):
                 raise ValueError(f"{name} must have shape {(cfg.batch, T, heads, cfg.head_dim)}, not {tuple(t.shape)}")
@@ -210,19 +214,31 @@ class Session:
         if tuple(out.shape) != (*rows, cfg.head_dim) or tuple(lse.shape) != rows:
             raise ValueError("out and lse must have the shapes of q and of its rows")
         n = B.swarm_tree_attn_workspace_bytes(self.shape, T)
-        if getattr(self, "_tree_ws", None) is None or self._tree_ws.numel() < n:
-            self._tree_ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-        self._allocated_for(stream, out, lse, self._tree_ws)
+        # one per size, kept as long as the session: a captured graph goes on using the one it was captured with
+        pool = self.__dict__.setdefault("_tree_workspaces", {})
+        if n not in pool:
+            pool[n] = torch.empty(n, dtype=torch.uint8, device=self.device)
+        workspace = pool[n]
+        self._allocated_for(stream, out, lse, workspace)
         tree = B.make_tree(q=q, k=k, v=v, n_draft=n_draft, mask=mask)
         sel, n_sel = (self.o.sel, self.o.n_sel) if selected else (None, None)
-        B.swarm_tree_attn(self.ctx, self.inputs, tree, sel, n_sel, self._tree_ws, out, lse, stream)
+        B.swarm_tree_attn(self.ctx, self.inputs, tree, sel, n_sel, workspace, out, lse, stream)
         return out, lse
+
+    def _about_to_write(self, stream) -> None:
+        """The cache's tables are about to change: nothing may still read them beside the stream."""
+        if self.index_prefetch:
+            raise ValueError("a Session with index_prefetch reads its index ahead of the stream: it cannot change")
+        if self.tail_stream is not None:
+            self.tail_join(stream)
 
     def append(self, k, v, n_new, path=None, stream=None) -> None:
         """swarm_append_tokens into the session's pool: the tokens (k / v [B, T, Hkv, d], all or the accepted ``path``), the
-        summaries of the pages they reach and the workload's context lengths, all in place."""
+        summaries of the pages they reach and the workload's context lengths, all in place.  The page2cluster entries of
+        pages that are reached for the first time are the caller's."""
         cfg = self.cfg
-        if tuple(k.shape) != (cfg.batch, k.shape[1], cfg.n_kv_heads, cfg.head_dim):
+        self._about_to_write(stream)
+        if k.dim() != 4 or tuple(k.shape) != (cfg.batch, k.shape[1], cfg.n_kv_heads, cfg.head_dim):
             raise ValueError(f"k must have shape {(cfg.batch, 'T', cfg.n_kv_heads, cfg.head_dim)}, not {tuple(k.shape)}")
         tokens = B.make_new_tokens(k=k, v=v, n_new=n_new, path=path)
         B.swarm_append_tokens(self.ctx, self.inputs, tokens, self.w.kv_pool, self.ksum, self.w.ctx_len, stream)
@@ -230,9 +246,13 @@ class Session:
     def compact(self, parent, reserve=None, keep=None, stream=None) -> None:
         """swarm_plan_pages and swarm_move_pages inside the session's pool: new request j continues old request parent[j]
         (strictly ascending over the requests that have one; -1: freed) with the pages that ``keep`` holds and reserve[j] spare
-        ones.  Moves K/V, summaries and page2cluster and writes the workload's page_base and ctx_len.  A plan that is refused
-        leaves everything as it was and shows in status()."""
+        ones.  Moves K/V, summaries and page2cluster, writes the workload's page_base and ctx_len, and moves the cluster tables
+        (cluster_base, replica masks, sizes) with their requests: global cluster ids change, sizes stay as they are where pages
+        are dropped.  A plan that is refused leaves everything as it was and shows in status()."""
         dev, n_pool = self.device, self.w.n_pool_pages
+        if hasattr(self, "medoid_index"):
+            raise ValueError("the medoid index lists pages by number: compact before enable_medoid_index()")
+        self._about_to_write(stream)
         if getattr(self, "_pages", None) is None:
             i32 = dict(dtype=torch.int32, device=dev)
             self._pages = dict(src=torch.empty(n_pool, **i32), dst=torch.empty(n_pool, **i32), n_moves=torch.empty(1, **i32),
@@ -251,8 +271,23 @@ class Session:
         B.swarm_plan_pages(self.ctx, plan, stream)
         B.swarm_move_pages(self.ctx, moves, t["ws"], stream)
         with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(dev)):
+            self._move_cluster_tables(parent, t["n_moves"] >= 0)
             self.w.page_base.copy_(t["base"])
             self.w.ctx_len.copy_(t["len"])
+
+    def _move_cluster_tables(self, parent, planned) -> None:
+        """Small tables, in step with page2cluster, whose ids are local to a request: request j has the clusters of old request
+        parent[j] (each old request at most once, so they fit where they were).  ``planned`` (on the device): there is a plan."""
+        w, n = self.w, parent.numel()
+        old = parent.long().clamp(0, n - 1)
+        sizes = torch.where(parent >= 0, w.cluster_base[old + 1] - w.cluster_base[old], 0)
+        base = torch.cat([torch.zeros_like(sizes[:1]), sizes.cumsum(0)])
+        at = torch.arange(w.n_clusters, device=self.device)
+        j = (torch.searchsorted(base, at, right=True) - 1).clamp(max=n - 1)
+        source = torch.where(planned & (at < base[-1]), w.cluster_base[old[j]] + at - base[j], at)
+        for table in (w.cluster_replica_mask, w.cluster_size):
+            table.copy_(table[source])
+        w.cluster_base.copy_(torch.where(planned, base, w.cluster_base))
 
     def status(self) -> int:
         return B.swarm_device_status(self.ctx)

@@ -436,3 +436,124 @@ def test_arguments_are_checked():
     assert e.value.code == B.ERR_INVALID_ARG
     close(lay.ctx)
     c.close()
+
+
+def test_captured_trees_keep_their_workspace():
+    """A graph of short trees, then calls with longer ones, whose workspace is larger: the graph's is still its own."""
+    cfg = small()
+    w = W.generate(cfg, seed=12, device=DEV)
+    s = Session(w)
+    gen = torch.Generator(device=DEV).manual_seed(8)
+
+    def drafts(T):
+        make = lambda heads: torch.randn((3, T, heads, 128), generator=gen, device=DEV).to(torch.bfloat16)   # noqa: E731
+        return make(cfg.n_q_heads), make(cfg.n_kv_heads), make(cfg.n_kv_heads), dev([T] * 3)
+
+    few, many = drafts(2), drafts(40)
+    want = s.tree_attn(*few)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        out, lse = s.tree_attn(*few)
+    first = s.tree_attn(*many)
+    junk = [torch.full((1 << 20,), -1, dtype=torch.int32, device=DEV) for _ in range(64)]
+    kept = [x.clone() for x in junk]
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    assert all(torch.equal(a, b) for a, b in zip(junk, kept))
+    again = s.tree_attn(*many)
+    torch.cuda.synchronize()
+    assert torch.equal(first[0], again[0]) and s.status() == 0
+    s.close()
+
+
+def test_clusters_move_with_their_requests():
+    """After a compaction the cluster tables are those of the requests that are left, and a resolution gives what it gave."""
+    cfg = small(batch=4, ctx_len=16 * 90 + 5)
+    w = W.generate(cfg, seed=31, device=DEV)
+    left = W.generate(cfg, seed=31, device=DEV)
+    s = Session(w)
+    tables = [x.clone() for x in (w.cluster_base, w.cluster_replica_mask, w.cluster_size, w.page2cluster)]
+    s.compact(dev([2, 1, 0, 3]))                                # refused: not in order
+    assert s.status() == B.DEV_BAD_PAGE
+    s.compact(dev([9, 1, 2, 3]))                                # refused: no such request
+    assert s.status() == B.DEV_BAD_PAGE
+    for now, was in zip((w.cluster_base, w.cluster_replica_mask, w.cluster_size, w.page2cluster), tables):
+        assert torch.equal(now, was)
+    s.compact(dev([1, -1, 2, 3]))
+    assert s.status() == 0
+    old = left.cluster_base.tolist()
+    n = [old[b + 1] - old[b] for b in range(4)]
+    base = [0, n[1], n[1], n[1] + n[2], n[1] + n[2] + n[3]]
+    assert w.cluster_base.tolist() == base
+    for j, b in ((0, 1), (2, 2), (3, 3)):
+        for now, was in ((w.cluster_replica_mask, left.cluster_replica_mask), (w.cluster_size, left.cluster_size)):
+            assert torch.equal(now[base[j]: base[j + 1]], was[old[b]: old[b + 1]])
+        lo, hi, P = int(w.page_base[j]), int(left.page_base[b]), int(left.page_base[b + 1] - left.page_base[b])
+        assert torch.equal(w.page2cluster[lo: lo + P], left.page2cluster[hi: hi + P])
+    # resolution of hand-made selections: of old requests 1, 2, 3 before, of new requests 0, 2, 3 behind
+    ref = Session(left)
+    sel = torch.randint(0, 90, (4, cfg.n_q_heads, cfg.top_k), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV,
+                        dtype=torch.int32)
+    count = torch.full((4, cfg.n_q_heads), cfg.top_k, dtype=torch.int32, device=DEV)
+    before, behind = count.clone(), count.clone()
+    before[0] = 0
+    behind[1] = 0
+    ref.resolve(sel[[0, 1, 2, 3]].contiguous(), before)
+    s.resolve(sel[[1, 0, 2, 3]].contiguous(), behind)
+    torch.cuda.synchronize()
+    assert s.status() == 0 and ref.status() == 0
+    m = int(ref.o.n_uniq[0])
+    assert int(s.o.n_uniq[0]) == m
+
+    def routed(o, starts, requests):
+        ids = [(r, c - starts[r], q) for c, q in zip(o.uniq[:m].tolist(), o.queue_of[:m].tolist())
+               for r in requests if starts[r] <= c < starts[r + 1]]
+        return {(requests.index(r), c): q for r, c, q in ids}
+
+    assert set(routed(ref.o, old, [1, 2, 3])) == set(routed(s.o, base, [0, 2, 3]))
+    assert sorted(routed(s.o, base, [0, 2, 3])) and torch.equal(ref.o.queue_load.sum(), s.o.queue_load.sum())
+    s.close()
+    ref.close()
+
+
+def test_tables_are_not_changed_under_a_reader():
+    cfg = small()
+    w = W.generate(cfg, seed=13, device=DEV)
+    s = Session(w, index_prefetch=True)
+    kv = torch.zeros((3, 1, cfg.n_kv_heads, 128), dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(ValueError, match="index_prefetch"):
+        s.append(kv, kv, dev([1, 1, 1]))
+    with pytest.raises(ValueError, match="index_prefetch"):
+        s.compact(dev([0, 1, 2]))
+    s.close()
+    # a resolution on a stream of its own is waited for
+    tail = torch.cuda.Stream()
+    a, b = Session(w), Session(W.generate(cfg, seed=13, device=DEV), tail_stream=tail)
+    a.step()
+    for _ in range(3):
+        b.step()
+        b.compact(dev([0, 1, 2]))
+    b.tail_join()
+    torch.cuda.synchronize()
+    for f in ("sel", "out", "queue_load", "n_uniq"):
+        assert torch.equal(getattr(a.o, f), getattr(b.o, f)), f
+    with pytest.raises(ValueError, match="medoid"):
+        a.enable_medoid_index(4)
+        a.compact(dev([0, 1, 2]))
+    a.close()
+    b.close()
+
+
+def test_counts_that_do_not_fit_are_refused():
+    lay = Layout([16], [1], 40, hkv=2)
+    src, dst, one = dev([1]), dev([2]), dev([1])
+    ws = torch.empty(B.swarm_move_pages_workspace_bytes(lay.shape), dtype=torch.uint8, device=DEV)
+    moves = B.make_page_moves(src=src, dst=dst, n_moves=one, from_pool=lay.pool, to_pool=lay.pool)
+    for n, code in ((0, B.ERR_INVALID_ARG), ((1 << 31) - 1, B.ERR_UNSUPPORTED), (1 << 30, B.ERR_UNSUPPORTED), ((1 << 30) - 1, B.ERR_UNSUPPORTED)):
+        moves.max_moves = n
+        with pytest.raises(B.SwarmError) as e:
+            B.swarm_move_pages(lay.ctx, moves, ws)
+        assert e.value.code == code
+    close(lay.ctx)
