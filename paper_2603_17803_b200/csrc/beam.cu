@@ -15,6 +15,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "swarm_internal.cuh"
 
@@ -143,15 +144,21 @@ __device__ __forceinline__ void rank_all(int n, int* s_rank, Greater&& greater, 
   if (tid < n) out(tid, s_rank[tid]);
 }
 
+constexpr int kStages = 2, kLineBytes = 33 * 16;
+__device__ __forceinline__ void copy_line(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+
 // A chunk is kPer tokens for each of kBeamThreads threads; a CTA takes `span` chunks of a row one after the other.
 template <class T, int kPer>
 __global__ void __launch_bounds__(kBeamThreads, kPer == 32 ? 3 : 4)
 beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__ keys, float2* __restrict__ sums) {
   constexpr int kVec = 16 / (int)sizeof(T), kVecs = kPer / kVec, kChunk = kBeamThreads * kPer;
   constexpr int kMany = 64;                                   // threads with a candidate that are gathered as they are
-  __shared__ key_t s_max[128];
   constexpr int kRoom = kMaxBeamKeep + 128 * kPer;
-  __shared__ key_t s_cand[kRoom];
+  extern __shared__ __align__(16) unsigned char s_raw[];      // [kStages][warp][kVecs][33] 16-byte lines, then the candidates
+  key_t* s_cand = reinterpret_cast<key_t*>(s_raw + kStages * kBeamThreads / 32 * kVecs * kLineBytes);
+  __shared__ key_t s_max[128];
   __shared__ key_t s_top[kMaxBeamKeep];
   __shared__ float2 s_red[kBeamThreads / 32];
   __shared__ key_t s_bound;
@@ -172,15 +179,29 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   const int n_whole = max(0, (int)min((long long)(stop - begin), (long long)(end - 32 - first) / (int)sizeof(T) - begin) / kChunk);
   const char* const start = first + ((long long)begin + tid * kVec) * (int)sizeof(T) - shift;
   const char* next = start;
-  uint4 raw[kVecs];
-  auto fetch = [&] {
-    if (shift == 0) {
-#pragma unroll
-      for (int i = 0; i < kVecs; ++i) raw[i] = ldg_nc_v4(next + i * kBeamThreads * 16);
-    } else {
+  // Chunks travel through shared memory by 16-byte asynchronous copies, kStages ahead; a warp reads only what its own lanes have
+  // copied (and, of a row that starts inside a line, the line behind).
+  auto line = [&](int stage, int i) { return s_raw + ((stage * (kBeamThreads / 32) + warp) * kVecs + i) * kLineBytes + lane * 16; };
+  auto fetch = [&](int stage, bool some) {
+    if (some) {
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
-        const uint4 lo = __ldg(reinterpret_cast<const uint4*>(next + i * kBeamThreads * 16)), hi = __ldg(reinterpret_cast<const uint4*>(next + i * kBeamThreads * 16 + 16));
+        copy_line(line(stage, i), next + i * kBeamThreads * 16);
+        if (shift != 0 && lane == 31) copy_line(line(stage, i) + 16, next + i * kBeamThreads * 16 + 16);
+      }
+      next += kChunk * (int)sizeof(T);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  auto chunk_of = [&](int stage, uint4 (&raw)[kVecs]) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) raw[i] = *reinterpret_cast<const uint4*>(line(stage, i));
+    if (shift != 0) {
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        const uint4 lo = raw[i], hi = *reinterpret_cast<const uint4*>(line(stage, i) + 16);
         uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
         if (shift & 4) {
 #pragma unroll
@@ -195,7 +216,7 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
                             __funnelshift_r(w[3], w[4], bits));
       }
     }
-    next += kChunk * (int)sizeof(T);
+    __syncwarp();                                             // all lanes have read: the stage may be written again
   };
   if (tid == 0) s_count = 0;
   float top = -INFINITY, sum = 0.f;                           // of this thread's logits so far
@@ -222,14 +243,19 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   // Where more come than there is room for (logits that rise along the row), the stretch is done again with a look at every chunk.
   bool over = false;
   for (bool careful = false;; careful = true) {
-  if (n_whole > 0) fetch();
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) fetch(i, i < n_whole);
+  int stage = 0;
   bool more = false;                                          // this thread has appended since the last ranking
   for (int at0 = begin, chunk = 0; at0 < stop; at0 += kChunk, ++chunk) {
     float x[kPer];
     if (chunk < n_whole) {
+      uint4 raw[kVecs];
+      chunk_of(stage, raw);
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) Element<T>::unpack(raw[i], x + i * kVec);
-      if (chunk + 1 < n_whole) fetch();                       // the next chunk is on its way meanwhile
+      fetch(stage, chunk + kStages < n_whole);
+      if (++stage == kStages) stage = 0;
     } else {
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
@@ -333,7 +359,9 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
     }
   }
   if (!__syncthreads_or(over)) break;
-  // once more, from the start
+  // once more, from the start (copies under way would still write to the ring)
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
   over = false;
   if (tid == 0) s_count = 0;
   top = floor_ = -INFINITY;
@@ -497,13 +525,42 @@ long long merge_smem(int beams, int chunks, int keep, int group) {
 }
 int merge_group(int beams, int chunks, int keep) { return merge_smem(beams, chunks, keep, 4) <= kMergeSmemMax ? 4 : 1; }
 
+template <class T, int kPer>
+constexpr int chunk_smem() {
+  return kStages * kBeamThreads / 32 * (kPer * (int)sizeof(T) / 16) * kLineBytes + (kMaxBeamKeep + 128 * kPer) * (int)sizeof(key_t);
+}
+template <class T, int kPer>
+cudaError_t launch_chunks_of(const BeamCall& c, const Cut& cut, key_t* keys, float2* sums, cudaStream_t st) {
+  const dim3 grid((unsigned)((long long)c.batch * c.n_beams * cut.stretches));
+  return launch_pdl(beam_chunk_kernel<T, kPer>, grid, dim3(kBeamThreads), (size_t)chunk_smem<T, kPer>(), st, true, c, cut.stretches,
+                    cut.span, keys, sums);
+}
+// The kernels' room in shared memory, once per device (each of these calls takes the host a microsecond or two).
+template <class T, int kPer>
+cudaError_t configure_chunks() {
+  return cudaFuncSetAttribute(beam_chunk_kernel<T, kPer>, cudaFuncAttributeMaxDynamicSharedMemorySize, chunk_smem<T, kPer>());
+}
+cudaError_t configure_beam() {
+  static std::atomic<unsigned long long> configured{0};       // a bit per device
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = device < 64 ? 1ull << device : 0ull;
+  if (configured.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMergeSmemMax);
+  if (e == cudaSuccess) e = configure_chunks<float, 16>();
+  if (e == cudaSuccess) e = configure_chunks<__nv_bfloat16, 16>();
+  if (e == cudaSuccess) e = configure_chunks<__nv_bfloat16, 32>();
+  if (e == cudaSuccess) e = configure_chunks<__half, 16>();
+  if (e == cudaSuccess) e = configure_chunks<__half, 32>();
+  if (e == cudaSuccess) configured.fetch_or(bit, std::memory_order_release);
+  return e;
+}
 template <class T>
 cudaError_t launch_chunks(const BeamCall& c, const Cut& cut, key_t* keys, float2* sums, cudaStream_t st) {
-  const dim3 grid((unsigned)((long long)c.batch * c.n_beams * cut.stretches));
   if constexpr (sizeof(T) == 2)
-    if (cut.per == 32)
-      return launch_pdl(beam_chunk_kernel<T, 32>, grid, dim3(kBeamThreads), 0, st, true, c, cut.stretches, cut.span, keys, sums);
-  return launch_pdl(beam_chunk_kernel<T, 16>, grid, dim3(kBeamThreads), 0, st, true, c, cut.stretches, cut.span, keys, sums);
+    if (cut.per == 32) return launch_chunks_of<T, 32>(c, cut, keys, sums, st);
+  return launch_chunks_of<T, 16>(c, cut, keys, sums, st);
 }
 
 constexpr int64_t align256(int64_t x) { return (x + 255) & ~int64_t(255); }
@@ -534,7 +591,7 @@ cudaError_t launch_beam_select(const BeamCall& c, void* workspace, cudaStream_t 
   float2* sums = reinterpret_cast<float2*>(static_cast<unsigned char*>(workspace) + align256(rows * cut.stretches * c.n_keep * 8));
   const int group = merge_group(c.n_beams, cut.stretches, c.n_keep);
   const size_t smem = (size_t)merge_smem(c.n_beams, cut.stretches, c.n_keep, group);
-  cudaError_t e = cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMergeSmemMax);
+  cudaError_t e = configure_beam();
   if (e != cudaSuccess) return e;
   e = c.dtype == SWARM_DTYPE_F32    ? launch_chunks<float>(c, cut, keys, sums, st)
       : c.dtype == SWARM_DTYPE_BF16 ? launch_chunks<__nv_bfloat16>(c, cut, keys, sums, st)
