@@ -379,18 +379,16 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   for (int o = 16; o >= 1; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
   if (lane == 0) s_red[warp] = make_float2(m, l);
   __syncthreads();
-  const int lists = c.n_beams * stretches;                    // of a prompt; their candidates lie by rank, then by list
-  const long long b = blockIdx.x / lists;
-  key_t* out = keys + b * lists * keep + (blockIdx.x - b * lists);
+  key_t* out = keys + (long long)blockIdx.x * keep;
   const int n = s_count;                                      // at most n_keep, in no order while fewer
   if (tid < keep) {
     if (tid < n) {
       const key_t k = s_cand[tid];
       int rank = 0;
       for (int j = 0; j < n; ++j) rank += s_cand[j] > k;
-      out[(long long)rank * lists] = k;
+      out[rank] = k;
     } else {
-      out[(long long)tid * lists] = 0;                                           // no such candidate (below the key of every logit)
+      out[tid] = 0;                                           // no such candidate (below the key of every logit)
     }
   }
   if (tid == 0) {
@@ -419,8 +417,6 @@ __device__ __forceinline__ bool before(const Cand& a, const Cand& b) { return a.
 
 constexpr int kHold = 4;                                    // candidates that a thread keeps in registers
 
-// Candidates are taken by rank, then by list: the best of all lists then stand in many groups of neighbouring threads, and the
-// n_keep-th largest of the groups' maxima is a bound that few others pass (32 x 16 lists of 16: 13 us by list, XX by rank).
 // The candidates' sums are compared as ordered images with the index behind; what a thread cannot hold it reads again.
 __global__ void __launch_bounds__(kMergeThreads)
 beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restrict__ keys, const float2* __restrict__ sums) {
@@ -433,17 +429,30 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
   __shared__ int s_count, s_rank[kMergeThreads];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int keep = c.n_keep, V = c.vocab;
-  const int lists = c.n_beams * chunks, total = lists * keep;
+  const int per_beam = chunks * keep, total = c.n_beams * per_beam;
   const key_t* list = keys + (long long)b * total;
   pdl_wait();
   pdl_launch_dependents();
+  // Place p of the candidates belongs to group p % groups of neighbouring threads; the candidates of a list stand in as many groups,
+  // and lists turned against one another, since few lists may hold most of what is chosen: then the n_keep-th largest of the
+  // groups' maxima is a bound that few others pass (32 x 16 lists of 32 in places by list: 13 us of this kernel, so XX).
+  const int groups = kMergeThreads / group;
+  auto place = [&](int i) { return i * kMergeThreads + tid % group * groups + tid / group; };
+  auto entry = [&](int p) {                                   // list * n_keep + rank of a place
+    const int l = p / keep;
+    return l * keep + (p - l * keep + l % keep * 11) % keep;
+  };
   key_t held[kHold];
 #pragma unroll
-  for (int i = 0; i < kHold; ++i) held[i] = tid + i * kMergeThreads < total ? list[tid + i * kMergeThreads] : 0;
+  for (int i = 0; i < kHold; ++i) held[i] = place(i) < total ? list[entry(place(i))] : 0;
   for (int k = tid; k < c.n_beams; k += kMergeThreads) s_score[k] = (double)c.score[b * c.n_beams + k];
+  const float2* const all_sums = sums + (long long)b * c.n_beams * chunks;
+  auto sum_of = [&](int k) { return k < c.n_beams && lane < chunks ? all_sums[(long long)k * chunks + lane] : make_float2(-INFINITY, 0.f); };
+  float2 ahead = sum_of(warp);
   for (int k = warp; k < c.n_beams; k += kMergeThreads / 32) {
-    const float2* mine = sums + ((long long)b * c.n_beams + k) * chunks;
-    const float2 first = lane < chunks ? mine[lane] : make_float2(-INFINITY, 0.f);
+    const float2* mine = all_sums + (long long)k * chunks;
+    const float2 first = ahead;
+    ahead = sum_of(k + kMergeThreads / 32);
     float m = first.x;
     for (int i = lane + 32; i < chunks; i += 32) m = fmaxf(m, mine[i].x);
 #pragma unroll
@@ -458,7 +467,7 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
   if (tid == 0) s_count = 0;
   __syncthreads();
   auto cand = [&](int i, key_t k) {
-    const int beam = i % lists / chunks;
+    const int beam = i / per_beam;
     Cand r;
     const double s = s_score[beam] + ((double)key_value(k) - s_base[beam]);
     r.value = k == 0 || !(s > -INFINITY) ? 0 : ordered(s + 0.0);
@@ -469,11 +478,11 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
 #pragma unroll
   for (int i = 0; i < kHold; ++i) {
     mine[i].value = 0;
-    if (tid + i * kMergeThreads < total) mine[i] = cand(tid + i * kMergeThreads, held[i]);
+    if (place(i) < total) mine[i] = cand(place(i), held[i]);
     if (mine[i].value != 0 && before(mine[i], best)) best = mine[i];
   }
-  for (int i = tid + kHold * kMergeThreads; i < total; i += kMergeThreads) {
-    const Cand r = cand(i, list[i]);
+  for (int p = place(kHold); p < total; p += kMergeThreads) {
+    const Cand r = cand(p, list[entry(p)]);
     if (r.value != 0 && before(r, best)) best = r;
   }
   // maxima of groups of threads, where the candidates above their n_keep-th largest fit: ranking costs the square of their number
@@ -483,15 +492,14 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
   }
   if (tid % group == 0) s_max[tid / group] = best;
   __syncthreads();
-  const int groups = kMergeThreads / group;
   rank_all<kMergeThreads>(groups, s_rank, [&](int j, int i) { return before(s_max[j], s_max[i]); }, [&](int i, int r) { if (r == keep - 1) s_bound = s_max[i]; });
   __syncthreads();
   const Cand bound = s_bound;
 #pragma unroll
   for (int i = 0; i < kHold; ++i)
     if (mine[i].value != 0 && !before(bound, mine[i])) s_cand[atomicAdd(&s_count, 1)] = mine[i];
-  for (int i = tid + kHold * kMergeThreads; i < total; i += kMergeThreads) {
-    const Cand r = cand(i, list[i]);
+  for (int p = place(kHold); p < total; p += kMergeThreads) {
+    const Cand r = cand(p, list[entry(p)]);
     if (r.value != 0 && !before(bound, r)) s_cand[atomicAdd(&s_count, 1)] = r;
   }
   __syncthreads();
