@@ -100,7 +100,7 @@ __device__ __forceinline__ pair_t mul2(pair_t a, pair_t b) {
   return r;
 }
 __device__ __forceinline__ float exp_fast(float t) { return exp2_fast(fmaf(t, kLog2eLow, t * kLog2e)); }   // e^t for t <= 0
-// sum of e^(x - ref) over the logits, all <= ref (the difference first: logits of the type's lowest value mask, too)
+// sum of e^(x - ref) over the logits, none far above ref (the difference first: logits of the type's lowest value mask, too)
 template <int n>
 __device__ __forceinline__ float sum_exp(const float (&x)[n], float ref) {
   const pair_t l = pair_of(kLog2e, kLog2e), low = pair_of(kLog2eLow, kLog2eLow), r = pair_of(-ref, -ref);
@@ -185,9 +185,10 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   auto fetch = [&](int stage, bool some) {
     if (some) {
 #pragma unroll
-      for (int i = 0; i < kVecs; ++i) {
-        copy_line(line(stage, i), next + i * kBeamThreads * 16);
-        if (shift != 0 && lane == 31) copy_line(line(stage, i) + 16, next + i * kBeamThreads * 16 + 16);
+      for (int i = 0; i < kVecs; ++i) copy_line(line(stage, i), next + i * kBeamThreads * 16);
+      if (shift != 0 && lane == 31) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) copy_line(line(stage, i) + 16, next + i * kBeamThreads * 16 + 16);
       }
       next += kChunk * (int)sizeof(T);
     }
@@ -219,7 +220,10 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
     __syncwarp();                                             // all lanes have read: the stage may be written again
   };
   if (tid == 0) s_count = 0;
-  float top = -INFINITY, sum = 0.f;                           // of this thread's logits so far
+  // Sum of e^(x - top) over this thread's logits so far.  top is raised only by logits that pass it by more than kSlack: the
+  // exponentials stay below e^kSlack.
+  constexpr float kSlack = 8.f;
+  float top = -INFINITY, sum = 0.f;
   float floor_ = -INFINITY;                                   // the least of the n_keep largest at the last ranking
   // Ranks the gathered candidates and keeps the n_keep largest.  Entered behind a barrier, left in front of one.
   auto rank = [&] {
@@ -264,11 +268,15 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
         for (int e = 0; e < kVec; ++e) x[i * kVec + e] = at + e < V ? Element<T>::one(first, at + e) : -INFINITY;
       }
     }
-    float best2[2] = {-INFINITY, -INFINITY};
+    float best4[4];                                           // of quarters of the thread's logits
 #pragma unroll
-    for (int e = 0; e < kPer; e += 2) best2[(e >> 1) & 1] = max3(best2[(e >> 1) & 1], x[e], x[e + 1]);
-    const float mine = fmaxf(best2[0], best2[1]);
-    if (mine > top) {
+    for (int z = 0; z < 4; ++z) {
+      best4[z] = fmaxf(x[z * kPer / 4], x[z * kPer / 4 + 1]);
+#pragma unroll
+      for (int e = 2; e < kPer / 4; e += 2) best4[z] = max3(best4[z], x[z * kPer / 4 + e], x[z * kPer / 4 + e + 1]);
+    }
+    const float mine = fmaxf(max3(best4[0], best4[1], best4[2]), best4[3]);
+    if (mine > top + kSlack) {                                // (-inf: any finite value)
       sum *= exp_fast(top - mine);                            // (0 * 2^-inf the first time)
       top = mine;
     }
@@ -287,12 +295,16 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
     if (!careful && chunk > 0) {
       if (__any_sync(0xFFFFFFFFu, mine > floor_)) {
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-          if (x[e] > floor_) {
-            const int at = atomicAdd(&s_count, 1);
-            if (at < kRoom) s_cand[at] = make_key(x[e], token(e));
-            else over = true;
-            more = true;
+        for (int z = 0; z < 4; ++z) {
+          if (!__any_sync(0xFFFFFFFFu, best4[z] > floor_)) continue;
+#pragma unroll
+          for (int e = z * kPer / 4; e < (z + 1) * kPer / 4; ++e) {
+            if (x[e] > floor_) {
+              const int at = atomicAdd(&s_count, 1);
+              if (at < kRoom) s_cand[at] = make_key(x[e], token(e));
+              else over = true;
+              more = true;
+            }
           }
         }
       }
