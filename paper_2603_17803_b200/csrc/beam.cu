@@ -447,7 +447,7 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
   pdl_launch_dependents();
   // Place p of the candidates belongs to group p % groups of neighbouring threads; the candidates of a list stand in as many groups,
   // and lists turned against one another, since few lists may hold most of what is chosen: then the n_keep-th largest of the
-  // groups' maxima is a bound that few others pass (32 x 16 lists of 32 in places by list: 13 us of this kernel, so XX).
+  // groups' maxima is a bound that few others pass (32 x 16 lists of 32: this kernel 16 us with the places in order, so 7).
   const int groups = kMergeThreads / group;
   auto place = [&](int i) { return i * kMergeThreads + tid % group * groups + tid / group; };
   auto entry = [&](int p) {                                   // list * n_keep + rank of a place
