@@ -270,6 +270,7 @@ __device__ __forceinline__ int tiles_of(int ctx, int nd) {
 template <bool kWide>
 __global__ void __launch_bounds__(kThreads, 1)
 tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_constant__ CUtensorMap pool_page,
+                 const __grid_constant__ CUtensorMap pool_page_half,
                  const __grid_constant__ CUtensorMap draft_k, const __grid_constant__ CUtensorMap draft_v,
                  const __grid_constant__ CUtensorMap queries, const TreeArgs a) {
   using L = Layout<kWide>;
@@ -453,9 +454,13 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
           const int per_tile = kTile / S, pages = min(per_tile, (s.ctx_tokens + S - 1) / S - t * per_tile);
           if (lane == 0) bar_expect(bar, (unsigned)(pages * S * kHeadDim * 2));
           __syncwarp();
-          if (lane < pages)
+          // K's rows have to lie at one distance through the whole tile, a half of the coordinates at a time; V enters the product 16
+          // tokens at a time, so that a page's V may stay together: fewer and larger copies (selected pages 80.0 -> 76.4 us)
+          if (lane < pages && which == 0)
             for (int h = 0; h < 2; ++h)
-              tma_load(dst + h * kHalfBytes + lane * S * 128, &pool_page, 0, 0, s.base + page, h, s.kv * 2 + which, bar);
+              tma_load(dst + h * kHalfBytes + lane * S * 128, &pool_page_half, 0, 0, s.base + page, h, s.kv * 2, bar);
+          else if (lane < pages)
+            tma_load(dst + lane * S * 256, &pool_page, 0, 0, s.base + page, 0, s.kv * 2 + 1, bar);
         }
         __syncwarp();
         ++issued;
@@ -505,11 +510,15 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
           mma_ss(tmem + st * kTile, qd + off, kd + off, mma_shape(false), k > 0, lead);
         }
       };
-      auto values = [&](int st, int sl, bool add) {          // O += P V
-        const uint64_t vd = operand(smem_addr(smem + L::kRing + sl * kTileBytes), kHalfBytes, 1024);
+      // O += P V.  V's halves lie apart through the whole tile, or, of selected pages, through a page; the offsets of 16 tokens are
+      // those of odd and even places.
+      auto values = [&](int st, int sl, bool by_page, bool add) {
+        const uint64_t vd = operand(smem_addr(smem + L::kRing + sl * kTileBytes), by_page ? S * 128 : kHalfBytes, 1024);
+        const uint32_t odd = by_page && S == 16 ? 4096 >> 4 : 2048 >> 4, even = by_page ? 8192 >> 4 : 4096 >> 4;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          mma_ts(tmem + 256 + st * kTile, tmem + st * kTile + k * 8, vd + (uint64_t)(k * 128), mma_shape(true), add || k > 0, lead);
+          mma_ts(tmem + 256 + st * kTile, tmem + st * kTile + k * 8, vd + (uint64_t)((k >> 1) * even + (k & 1) * odd), mma_shape(true),
+                 add || k > 0, lead);
       };
       auto commit = [&](uint64_t* bar) { tc_commit(bar, lead); };
       // V rows behind the tile's last token may hold anything, and 0 * NaN must not reach the sums
@@ -517,8 +526,12 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
         const int left = t < s.ctx_tiles ? s.ctx_tokens - t * kTile : s.nd - (t - s.ctx_tiles) * kTile;
         if (left >= kTile) return;
         unsigned char* v = smem + L::kRing + sl * kTileBytes;
-        for (int i = lane; i < (kTile - left) * 16; i += 32)
-          *reinterpret_cast<uint4*>(v + ((i >> 3) & 1) * kHalfBytes + (left + (i >> 4)) * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+        const int rows = a.list != nullptr && t < s.ctx_tiles ? S : kTile;   // (16, 32 or 128) of a block whose halves lie apart
+        for (int i = lane; i < (kTile - left) * 16; i += 32) {
+          const int token = left + (i >> 4);
+          *reinterpret_cast<uint4*>(v + (token & -rows) * 256 + ((i >> 3) & 1) * rows * 128 + (token & (rows - 1)) * 128 + (i & 7) * 16) =
+              make_uint4(0, 0, 0, 0);
+        }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
       };
@@ -553,7 +566,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap pool_tile, const __grid_con
             p_phase ^= 1u << st;
             if (!ok) break;
             tc_fence_after();
-            values(st, sv, tv >= (wide ? 1 : 2));
+            values(st, sv, a.list != nullptr && s.t0 + tv < s.ctx_tiles, tv >= (wide ? 1 : 2));
             if (closes) commit(empty + sv);
           }
           if (has_k) {
@@ -964,8 +977,8 @@ tree_list_kernel(const TreeArgs a, const int32_t* __restrict__ sel, const int32_
   const int S = a.geo.S, len = a.ctx_len[b];
   const long long owned = a.page_base[b + 1] - a.page_base[b];
   const int P = len < 0 || pages_of(len, S) > owned ? 0 : min(pages_of(len, S), a.geo.Pmax);
-  // every selected page of the group's heads: kHold entries of a thread at a time, all loads ahead of their uses (one after the
-  // other they took 5 of the 8 us of 4 heads with 256 pages); the first ones are kept for the second look
+  // every selected page of the group's heads: kHold entries of a thread at a time, all loads ahead of their uses (4 heads with 256
+  // pages: 6.1 us, one after the other 8.3); the first ones are kept for the second look
   const int k = a.geo.k, entries = a.geo.g * k;
   constexpr int kHold = 8, kNone = -1;
   auto pages_at = [&](int j0, int (&p)[kHold]) {
@@ -1125,12 +1138,18 @@ cudaError_t launch_tree_attn(const Geometry& geo, const TreeCall& c, void* works
 
   const cuuint64_t row = kHeadDim * 2, S = (cuuint64_t)geo.S, Hkv = (cuuint64_t)geo.Hkv, T = (cuuint64_t)c.T;
   // pool: (64 coordinates, token of the page, page, half of the coordinates, KV head and K or V)
-  CUtensorMap tile, page, dk, dv, dq;
+  CUtensorMap tile{}, page{}, half{}, dk, dv, dq;
   const cuuint64_t pool_dims[5] = {64, S, (cuuint64_t)geo.n_pool_pages, 2, Hkv * 2};
   const cuuint64_t pool_strides[4] = {row, Hkv * 2 * S * row, 128, S * row};
-  const cuuint32_t tile_box[5] = {64, (cuuint32_t)S, (cuuint32_t)(kTile / S), 2, 1}, page_box[5] = {64, (cuuint32_t)S, 1, 1, 1};
-  cudaError_t e = make_map(&tile, c.kv_pool, pool_dims, pool_strides, tile_box);
-  if (e == cudaSuccess) e = make_map(&page, c.kv_pool, pool_dims, pool_strides, page_box);
+  const cuuint32_t tile_box[5] = {64, (cuuint32_t)S, (cuuint32_t)(kTile / S), 2, 1}, page_box[5] = {64, (cuuint32_t)S, 1, 2, 1},
+                   half_box[5] = {64, (cuuint32_t)S, 1, 1, 1};
+  cudaError_t e = cudaSuccess;                               // (each of these calls is host time in front of the launch)
+  if (c.sel == nullptr) {
+    e = make_map(&tile, c.kv_pool, pool_dims, pool_strides, tile_box);
+  } else {
+    e = make_map(&page, c.kv_pool, pool_dims, pool_strides, page_box);
+    if (e == cudaSuccess) e = make_map(&half, c.kv_pool, pool_dims, pool_strides, half_box);
+  }
   // drafted tokens: (64 coordinates, token, half of the coordinates, KV head, request)
   const cuuint64_t draft_dims[5] = {64, T, 2, Hkv, (cuuint64_t)geo.B};
   const cuuint64_t draft_strides[4] = {Hkv * row, 128, row, T * Hkv * row};
@@ -1159,8 +1178,8 @@ cudaError_t launch_tree_attn(const Geometry& geo, const TreeCall& c, void* works
   const int64_t most = (int64_t)geo.B * geo.Hkv * (((int64_t)geo.Pmax * geo.S + kTile - 1) / kTile + (c.T + kTile - 1) / kTile);
   a.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kMaxTreeCtas, sm_count()) / a.row_blocks, most));
   const unsigned grid = (unsigned)(a.chunks * a.row_blocks);
-  e = wide ? launch_pdl(tree_attn_kernel<true>, dim3(grid), dim3(kThreads), (size_t)Layout<true>::kBytes, st, true, tile, page, dk, dv, dq, a)
-           : launch_pdl(tree_attn_kernel<false>, dim3(grid), dim3(kThreads), (size_t)Layout<false>::kBytes, st, true, tile, page, dk, dv, dq, a);
+  e = wide ? launch_pdl(tree_attn_kernel<true>, dim3(grid), dim3(kThreads), (size_t)Layout<true>::kBytes, st, true, tile, page, half, dk, dv, dq, a)
+           : launch_pdl(tree_attn_kernel<false>, dim3(grid), dim3(kThreads), (size_t)Layout<false>::kBytes, st, true, tile, page, half, dk, dv, dq, a);
   if (e != cudaSuccess) return e;
   const int groups = (std::min(c.T, a.tile_tokens) * geo.g + 31) / 32;
   // few units are cut into many parts: their partials are shared by the warps of a CTA
