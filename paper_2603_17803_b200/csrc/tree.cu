@@ -17,7 +17,15 @@
 // sums are joined at the end through tensor memory; beyond (kWide), each has 128 rows of its own and both use every tile.
 //
 // The tiles of all (request, KV head) units form one list that is cut evenly over the CTAs, whatever the lengths
-// are; a unit that is cut leaves partial (m, l, O) per CTA, joined by a second kernel with a warp per row.
+// are; a unit that is cut leaves partial (m, l, O) per CTA, joined by a second kernel with a lane per row.
+//
+// What bounds it.  Up to 128 rows, HBM: 16 tokens x 4 heads over 128K tokens (537 MB) take 90 us, 6.0 TB/s.  More rows, the chain of a
+// tile: product, scores to registers, maximum, exponentials, P back, product.  Two streams overlap theirs, and the tensor cores work
+// 55 % of the time: 64 tokens x 8 heads over 256K tokens (550 GFLOP) take 495 us, 1.11 PFLOP/s at full clocks (570 us where the power
+// limit holds the clock at 1.45 GHz).  Leaving out half of the scores' products gained 7 % there, of O's products 3 %, the exponentials
+// 8 %: no unit by itself.  Selected pages: 8 x 16 tokens over 256 pages a head (338 MB) take 76 us, of which 6 build the lists; the
+// copies are of 2 KB (K) and 4 KB (V), with larger ones it would be 71.  A short prompt (777 tokens) takes 10 us: two launches, a
+// first tile from DRAM, the chain of two tiles, and the joining.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -57,7 +65,7 @@ struct Seg {                                               // tiles [t0, t1) of 
 template <bool kWide>
 struct Layout {
   static constexpr int kQTiles = kWide ? 2 : 1;
-  static constexpr int kSlots = 4;                           // more leave too little L1 (6 and 5: up to 5 % slower)
+  static constexpr int kSlots = 4;                           // 128 KB in flight; more leave too little L1 (6 and 5: up to 5 % slower)
   static constexpr int kRows = kQTiles * kTile;
   static constexpr int kRing = kQTiles * kTileBytes;
   static constexpr int kBars = kRing + kSlots * kTileBytes;
@@ -199,8 +207,8 @@ __device__ __forceinline__ pair_t add2(pair_t a, pair_t b) {
 }
 // 2^y of both for y > -126: y = n + f with n whole and |f| <= 1/2, 2^f by a polynomial of degree 5 (fitted to the least largest
 // relative error, 2.1e-7 in fp32), n added to the exponent.  It runs on the multiply-add units, beside the exponentials of the
-// special function unit (kByFma: which pairs of eight), which a tile of 256 rows would keep busy for longer than its K and V
-// take to arrive.
+// special function unit (kByFma: which pairs of eight; a quarter of them is best by 2 % among none to all), which a tile of 256
+// rows would keep busy for longer than its K and V take to arrive.
 constexpr unsigned kByFma = 0x11u;
 __device__ __forceinline__ void exp2_pair(pair_t y, float& lo, float& hi) {
   float y0, y1;
