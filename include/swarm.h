@@ -530,8 +530,8 @@ int32_t swarm_move_pages(swarm_ctx* ctx, const swarm_page_moves* moves, void* wo
  * Logits must be below +inf.  logits: SWARM_DTYPE_*, row (b, k) starts (b * n_beams + k) * row_stride elements behind the
  * first (row_stride >= vocab).  score f32 [batch][n_beams]; outputs [batch][n_keep]; 1 <= n_keep <= 64.
  * workspace: swarm_beam_select_workspace_bytes bytes of device memory (contents irrelevant), used by one call at a time;
- * < 0: minus an error code.  SWARM_ERR_UNSUPPORTED: vocab >= 2^30, n_beams * vocab >= 2^31, or too many candidates
- * (n_beams * vocab / 8192 * n_keep^2 beyond about 6 million). */
+ * < 0: minus an error code.  SWARM_ERR_UNSUPPORTED: vocab >= 2^30, n_beams * vocab >= 2^31, or n_beams * n_keep^2
+ * beyond about 2.9 million. */
 int64_t swarm_beam_select_workspace_bytes(int32_t batch, int32_t n_beams, int32_t vocab, int32_t n_keep);
 int32_t swarm_beam_select(const void* logits, int32_t dtype, int64_t row_stride, const float* score, int32_t batch,
                           int32_t n_beams, int32_t vocab, int32_t n_keep, void* workspace, int64_t workspace_bytes,

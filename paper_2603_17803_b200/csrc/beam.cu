@@ -14,7 +14,7 @@
 //
 // Bound by HBM while the rows are read: 32 x 16 rows of 131072 fp32 (268 MB) take 62 us, of which 46 at 5.8 TB/s, 9 while only the
 // SMs with a fourth row still read (512 rows on 148 SMs; shorter stretches balance them but pay a first chunk each: 72 us with
-// two per row), 7 the second kernel, a chain of barriers.  A prompt of 4 x 32000 takes 9.5: two launches, and those chains.
+// two per row), 7 the second kernel, a chain of barriers.  A prompt of 4 x 32000 takes 9: two launches, and those chains.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -27,7 +27,6 @@ namespace swarm {
 namespace {
 
 constexpr int kBeamThreads = 256;
-constexpr int kMergeThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 
 typedef unsigned long long key_t;
@@ -362,10 +361,14 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
     }
     if (__any_sync(0xFFFFFFFFu, mine > floor_ && mine >= bound_value)) {
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        if (__any_sync(0xFFFFFFFFu, x[e] > floor_)) {
-          const key_t k = make_key(x[e], token(e));
-          if (x[e] > floor_ && k >= bound) s_cand[atomicAdd(&s_count, 1)] = k;
+      for (int z = 0; z < 4; ++z) {
+        if (!__any_sync(0xFFFFFFFFu, best4[z] > floor_ && best4[z] >= bound_value)) continue;
+#pragma unroll
+        for (int e = z * kPer / 4; e < (z + 1) * kPer / 4; ++e) {
+          if (x[e] > floor_ && x[e] >= bound_value) {
+            const key_t k = make_key(x[e], token(e));
+            if (k >= bound) s_cand[atomicAdd(&s_count, 1)] = k;
+          }
         }
       }
     }
@@ -435,26 +438,27 @@ __device__ __forceinline__ bool before(const Cand& a, const Cand& b) { return a.
 constexpr int kHold = 4;                                    // candidates that a thread keeps in registers
 
 // The candidates' sums are compared as ordered images with the index behind; what a thread cannot hold it reads again.
-__global__ void __launch_bounds__(kMergeThreads)
-beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restrict__ keys, const float2* __restrict__ sums) {
+template <int kThreads, int kGroups>
+__global__ void __launch_bounds__(kThreads)
+beam_merge_kernel(const BeamCall c, int chunks, const key_t* __restrict__ keys, const float2* __restrict__ sums) {
   extern __shared__ __align__(16) unsigned char smem[];
   double* s_base = reinterpret_cast<double*>(smem);           // [n_beams] log sum exp, then [n_beams] scores
   double* s_score = s_base + c.n_beams;
   Cand* s_max = reinterpret_cast<Cand*>(s_score + c.n_beams);
-  Cand* s_cand = s_max + kMergeThreads;
+  Cand* s_cand = s_max + kGroups;
   __shared__ Cand s_bound;
-  __shared__ int s_count, s_rank[kMergeThreads];
+  __shared__ int s_count, s_rank[kThreads];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int keep = c.n_keep, V = c.vocab;
   const int per_beam = chunks * keep, total = c.n_beams * per_beam;
   const key_t* list = keys + (long long)b * total;
   pdl_wait();
   pdl_launch_dependents();
-  // Place p of the candidates belongs to group p % groups of neighbouring threads; the candidates of a list stand in as many groups,
+  // Place p of the candidates belongs to group p % kGroups of neighbouring threads; the candidates of a list stand in as many groups,
   // and lists turned against one another, since few lists may hold most of what is chosen: then the n_keep-th largest of the
-  // groups' maxima is a bound that few others pass (32 x 16 lists of 32: this kernel 16 us with the places in order, so 7).
-  const int groups = kMergeThreads / group;
-  auto place = [&](int i) { return i * kMergeThreads + tid % group * groups + tid / group; };
+  // groups' maxima is a bound that few others pass (32 x 16 lists of 32: this kernel 16 us with the places in order, 7 so).
+  constexpr int kGroup = kThreads / kGroups;
+  auto place = [&](int i) { return i * kThreads + tid % kGroup * kGroups + tid / kGroup; };
   auto entry = [&](int p) {                                   // list * n_keep + rank of a place
     const int l = p / keep;
     return l * keep + (p - l * keep + l % keep * 11) % keep;
@@ -462,14 +466,14 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
   key_t held[kHold];
 #pragma unroll
   for (int i = 0; i < kHold; ++i) held[i] = place(i) < total ? list[entry(place(i))] : 0;
-  for (int k = tid; k < c.n_beams; k += kMergeThreads) s_score[k] = (double)c.score[b * c.n_beams + k];
+  for (int k = tid; k < c.n_beams; k += kThreads) s_score[k] = (double)c.score[b * c.n_beams + k];
   const float2* const all_sums = sums + (long long)b * c.n_beams * chunks;
   auto sum_of = [&](int k) { return k < c.n_beams && lane < chunks ? all_sums[(long long)k * chunks + lane] : make_float2(-INFINITY, 0.f); };
   float2 ahead = sum_of(warp);
-  for (int k = warp; k < c.n_beams; k += kMergeThreads / 32) {
+  for (int k = warp; k < c.n_beams; k += kThreads / 32) {
     const float2* mine = all_sums + (long long)k * chunks;
     const float2 first = ahead;
-    ahead = sum_of(k + kMergeThreads / 32);
+    ahead = sum_of(k + kThreads / 32);
     float m = first.x;
     for (int i = lane + 32; i < chunks; i += 32) m = fmaxf(m, mine[i].x);
 #pragma unroll
@@ -498,24 +502,24 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
     if (place(i) < total) mine[i] = cand(place(i), held[i]);
     if (mine[i].value != 0 && before(mine[i], best)) best = mine[i];
   }
-  for (int p = place(kHold); p < total; p += kMergeThreads) {
+  for (int p = place(kHold); p < total; p += kThreads) {
     const Cand r = cand(p, list[entry(p)]);
     if (r.value != 0 && before(r, best)) best = r;
   }
   // maxima of groups of threads, where the candidates above their n_keep-th largest fit: ranking costs the square of their number
-  for (int o = 1; o < group; o <<= 1) {
+  for (int o = 1; o < kGroup; o <<= 1) {
     const Cand other{__shfl_xor_sync(0xFFFFFFFFu, best.value, o), __shfl_xor_sync(0xFFFFFFFFu, best.index, o)};
     if (before(other, best)) best = other;
   }
-  if (tid % group == 0) s_max[tid / group] = best;
+  if (tid % kGroup == 0) s_max[tid / kGroup] = best;
   __syncthreads();
-  rank_all<kMergeThreads>(groups, s_rank, [&](int j, int i) { return before(s_max[j], s_max[i]); }, [&](int i, int r) { if (r == keep - 1) s_bound = s_max[i]; });
+  rank_all<kThreads>(kGroups, s_rank, [&](int j, int i) { return before(s_max[j], s_max[i]); }, [&](int i, int r) { if (r == keep - 1) s_bound = s_max[i]; });
   __syncthreads();
   const Cand bound = s_bound;
 #pragma unroll
   for (int i = 0; i < kHold; ++i)
     if (mine[i].value != 0 && !before(bound, mine[i])) s_cand[atomicAdd(&s_count, 1)] = mine[i];
-  for (int p = place(kHold); p < total; p += kMergeThreads) {
+  for (int p = place(kHold); p < total; p += kThreads) {
     const Cand r = cand(p, list[entry(p)]);
     if (r.value != 0 && !before(bound, r)) s_cand[atomicAdd(&s_count, 1)] = r;
   }
@@ -529,12 +533,13 @@ beam_merge_kernel(const BeamCall c, int chunks, int group, const key_t* __restri
     c.token[at] = some ? (int)(r.index % (uint32_t)V) : -1;
   };
   if (tid >= n && tid < keep) write(Cand{0, 0}, tid);
-  rank_all<kMergeThreads>(n, s_rank, [&](int j, int i) { return before(s_cand[j], s_cand[i]); }, [&](int i, int r) { if (r < keep) write(s_cand[i], r); });
+  rank_all<kThreads>(n, s_rank, [&](int j, int i) { return before(s_cand[j], s_cand[i]); }, [&](int i, int r) { if (r < keep) write(s_cand[i], r); });
 }
 
-// How a row is cut.  Elements per thread: 64 bytes of them (with the next 64 on their way), of 16-bit types 32 bytes where that
-// leaves SMs without a chunk.  Chunks per CTA: as many as leave three CTAs per SM, since the candidates grow rare with the length of a
-// stretch (32 x 16 x 131072 fp32: 62 us with whole rows, 72 with halves, 83 with quarters).
+// How a row is cut.  Elements per thread: 64 bytes of them, of 16-bit types 32 bytes where that leaves SMs without a chunk.
+// Stretches: as many as the device holds CTAs at a time, since candidates grow rare with the length of a stretch and each pays for a
+// first chunk (fp32, 32 x 16 x 131072: 62 us with whole rows, 72 with halves, 83 with quarters; bf16, 5 x 16 x 119450: 25 us with 5
+// stretches in one wave, 40 with 8 in two).
 struct Cut {
   int per, span, stretches;
 };
@@ -542,17 +547,21 @@ Cut cut_of(long long rows, int vocab, int dtype) {
   Cut c;
   auto chunks = [&](int per) { return (vocab + kBeamThreads * per - 1) / (kBeamThreads * per); };
   c.per = dtype == SWARM_DTYPE_F32 || rows * chunks(32) < 148 ? 16 : 32;
-  c.span = (int)std::max<long long>(1, std::min<long long>(32, rows * chunks(c.per) / (148 * 3)));
+  const long long at_once = 148 * (c.per == 32 ? 3 : 4);
+  const int most = (int)std::max<long long>(1, std::min<long long>(chunks(c.per), at_once / rows));
+  c.span = (chunks(c.per) + most - 1) / most;
   c.stretches = (chunks(c.per) + c.span - 1) / c.span;
   return c;
 }
+// The second kernel: 64 groups of candidates where all of the n_keep best groups' candidates fit in shared memory, else 256; four
+// candidates per thread of 256 threads, or, of more, of 1024 (bf16, 5 x 16 x 119450, 2560 candidates: 7 us of this kernel, 11 with 256).
 constexpr int kMergeSmemMax = 200 * 1024;
-// Shared memory of the second kernel: every thread of the n_keep groups above the bound may bring all of its candidates.
-long long merge_smem(int beams, int chunks, int keep, int group) {
-  const long long total = (long long)beams * chunks * keep, per = (total + kMergeThreads - 1) / kMergeThreads;
-  return beams * 16LL + (kMergeThreads + std::min(keep * per * group, total)) * (long long)sizeof(Cand);
+long long candidates(int beams, int stretches, int keep) { return (long long)beams * stretches * keep; }
+long long merge_smem(int beams, int stretches, int keep, int groups) {
+  const long long total = candidates(beams, stretches, keep);
+  return beams * 16LL + (groups + std::min(keep * ((total + groups - 1) / groups), total)) * (long long)sizeof(Cand);
 }
-int merge_group(int beams, int chunks, int keep) { return merge_smem(beams, chunks, keep, 4) <= kMergeSmemMax ? 4 : 1; }
+int merge_groups(int beams, int stretches, int keep) { return merge_smem(beams, stretches, keep, 64) <= kMergeSmemMax ? 64 : 256; }
 
 template <class T, int kPer>
 constexpr int chunk_smem() {
@@ -576,7 +585,9 @@ cudaError_t configure_beam() {
   if (e != cudaSuccess) return e;
   const unsigned long long bit = device < 64 ? 1ull << device : 0ull;
   if (configured.load(std::memory_order_acquire) & bit) return cudaSuccess;
-  e = cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMergeSmemMax);
+  e = cudaFuncSetAttribute(beam_merge_kernel<256, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMergeSmemMax);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(beam_merge_kernel<1024, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMergeSmemMax);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(beam_merge_kernel<1024, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMergeSmemMax);
   if (e == cudaSuccess) e = configure_chunks<float, 16>();
   if (e == cudaSuccess) e = configure_chunks<__nv_bfloat16, 16>();
   if (e == cudaSuccess) e = configure_chunks<__nv_bfloat16, 32>();
@@ -605,7 +616,7 @@ bool beam_supported(int batch, int n_beams, int vocab, int n_keep) {
   const long long rows = (long long)batch * n_beams;
   const int parts = most_stretches(rows, vocab);
   return (long long)n_beams * vocab < (1LL << 31) && rows * parts < (1LL << 31) && (long long)n_beams * parts * n_keep < (1LL << 30) &&
-         merge_smem(n_beams, parts, n_keep, 1) <= kMergeSmemMax;
+         merge_smem(n_beams, parts, n_keep, 256) <= kMergeSmemMax;
 }
 
 long long beam_select_workspace_bytes(int batch, int n_beams, int vocab, int n_keep) {
@@ -618,15 +629,17 @@ cudaError_t launch_beam_select(const BeamCall& c, void* workspace, cudaStream_t 
   const Cut cut = cut_of(rows, c.vocab, c.dtype);
   key_t* keys = static_cast<key_t*>(workspace);
   float2* sums = reinterpret_cast<float2*>(static_cast<unsigned char*>(workspace) + align256(rows * cut.stretches * c.n_keep * 8));
-  const int group = merge_group(c.n_beams, cut.stretches, c.n_keep);
-  const size_t smem = (size_t)merge_smem(c.n_beams, cut.stretches, c.n_keep, group);
+  const int groups = merge_groups(c.n_beams, cut.stretches, c.n_keep);
+  const size_t smem = (size_t)merge_smem(c.n_beams, cut.stretches, c.n_keep, groups);
   cudaError_t e = configure_beam();
   if (e != cudaSuccess) return e;
   e = c.dtype == SWARM_DTYPE_F32    ? launch_chunks<float>(c, cut, keys, sums, st)
       : c.dtype == SWARM_DTYPE_BF16 ? launch_chunks<__nv_bfloat16>(c, cut, keys, sums, st)
                                     : launch_chunks<__half>(c, cut, keys, sums, st);
   if (e != cudaSuccess) return e;
-  return launch_pdl(beam_merge_kernel, dim3((unsigned)c.batch), dim3(kMergeThreads), smem, st, true, c, cut.stretches, group, keys, sums);
+  const bool many = groups > 64 || candidates(c.n_beams, cut.stretches, c.n_keep) > kHold * 256;
+  auto* merge = !many ? beam_merge_kernel<256, 64> : groups == 64 ? beam_merge_kernel<1024, 64> : beam_merge_kernel<1024, 256>;
+  return launch_pdl(merge, dim3((unsigned)c.batch), dim3(many ? 1024 : 256), smem, st, true, c, cut.stretches, keys, sums);
 }
 
 }  // namespace swarm

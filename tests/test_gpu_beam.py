@@ -169,3 +169,29 @@ def test_refusals():
     with pytest.raises(B.SwarmError) as e:
         B.swarm_beam_select(f, score, ws[:16], torch.zeros((1, 4), device=DEV), i, i.clone())
     assert e.value.code == B.ERR_WORKSPACE_TOO_SMALL
+
+
+@pytest.mark.parametrize("batch,beams,V,keep,dtype", [
+    (1, 16, 131072, 64, torch.float32), (5, 16, 119450, 32, torch.bfloat16), (2, 7, 40001, 40, torch.float16), (3, 1, 250007, 64, torch.bfloat16)])
+def test_many_candidates_for_a_prompt(batch, beams, V, keep, dtype):
+    """Rows cut into many stretches: thousands to tens of thousands of candidates are left to the second kernel, many of equal value,
+    once spread over the beams and once all of them in two."""
+    gen = torch.Generator(device=DEV).manual_seed(V)
+    logits = (torch.randn((batch, beams, V), generator=gen, device=DEV) * 3).round().to(dtype)
+    check(logits, torch.zeros((batch, beams), device=DEV), keep)
+    logits = (torch.randn((batch, beams, V), generator=gen, device=DEV) * 3).to(dtype)
+    score = torch.full((batch, beams), -30.0, device=DEV)
+    score[:, -1] = -1.0
+    score[:, 0] = -1.25
+    check(logits, score, keep)
+
+
+@pytest.mark.parametrize("order", ["rising", "falling", "random"])
+def test_whole_rows_in_a_stretch(order):
+    """More rows than the device holds CTAs: each is one stretch."""
+    gen = torch.Generator(device=DEV).manual_seed(23)
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.randn((330, 2, 36865), generator=gen, device=DEV) * 4
+        if order != "random":
+            x = x.sort(-1, descending=order == "falling").values
+        check(x.to(dtype), -torch.rand((330, 2), generator=gen, device=DEV), 33)
