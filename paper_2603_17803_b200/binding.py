@@ -106,7 +106,7 @@ def _ptr(t: Optional[torch.Tensor], name: str = "tensor", device_check: bool = T
 
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:      # (building torch's stream object costs as much as a launch: 3.6 against 0.3 us)
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -432,7 +432,7 @@ class swarm_tree(ctypes.Structure):
 
 
 def _expect(t: torch.Tensor, name: str, dtype, shape) -> None:
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype != dtype or t.shape != shape:                # (torch.Size is a tuple)
         raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
 
 
@@ -593,9 +593,11 @@ def swarm_beam_select(logits: torch.Tensor, score: torch.Tensor, workspace: torc
     if logits.dtype not in _LOGIT_TYPES or logits.dim() != 3:
         raise ValueError("logits must be a float32, bfloat16 or float16 tensor of three dimensions")
     batch, beams, vocab = logits.shape
-    if not logits.is_cuda or logits.get_device() != torch.cuda.current_device():
+    if not logits.is_cuda or logits.get_device() != torch._C._cuda_getDevice():
         raise ValueError("logits must be a CUDA tensor on the current device")
     pitch = logits.stride(1) if beams > 1 else logits.stride(0) if batch > 1 else vocab
+    if vocab >> 31:
+        raise ValueError("a row must have fewer than 2^31 logits")
     if logits.stride(2) != 1 and vocab > 1 or pitch < vocab or (batch > 1 and logits.stride(0) != beams * pitch):
         raise ValueError("logits must have contiguous rows at one distance")
     keep = new_score.shape[-1]
@@ -603,9 +605,9 @@ def swarm_beam_select(logits: torch.Tensor, score: torch.Tensor, workspace: torc
     _expect(new_score, "new_score", torch.float32, (batch, keep))
     _expect(parent, "parent", torch.int32, (batch, keep))
     _expect(token, "token", torch.int32, (batch, keep))
-    rc = load_library().swarm_beam_select(ctypes.c_void_p(logits.data_ptr()), ctypes.c_int32(_LOGIT_TYPES[logits.dtype]),
-                                          ctypes.c_int64(pitch), _ptr(score, "score"), ctypes.c_int32(batch), ctypes.c_int32(beams),
-                                          ctypes.c_int32(vocab), ctypes.c_int32(keep), _ptr(workspace, "workspace"),
+    # (a Python int is passed as a C int: no wrapper to build for the 32-bit arguments)
+    rc = load_library().swarm_beam_select(ctypes.c_void_p(logits.data_ptr()), _LOGIT_TYPES[logits.dtype], ctypes.c_int64(pitch),
+                                          _ptr(score, "score"), batch, beams, vocab, keep, _ptr(workspace, "workspace"),
                                           ctypes.c_int64(workspace.numel() * workspace.element_size()),
                                           _ptr(new_score, "new_score"), _ptr(parent, "parent"), _ptr(token, "token"),
                                           _stream(stream))
