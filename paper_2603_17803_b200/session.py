@@ -286,7 +286,7 @@ class Session:
         j = (torch.searchsorted(base, at, right=True) - 1).clamp(max=n - 1)
         source = torch.where(planned & (at < base[-1]), w.cluster_base[old[j]] + at - base[j], at)
         for table in (w.cluster_replica_mask, w.cluster_size):
-            table.copy_(table[source])
+            table[: w.n_clusters].copy_(table[source])
         w.cluster_base.copy_(torch.where(planned, base, w.cluster_base))
 
     def status(self) -> int:
