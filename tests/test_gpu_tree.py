@@ -171,3 +171,27 @@ def test_tree_attention_matches_the_formula(name):
     c.check()
     assert B.swarm_device_status(c.ctx) == 0
     c.close()
+
+
+MANY = {
+    # a thread looks after several units
+    "units_beyond_threads": dict(lens=[(53 * i) % 200 for i in range(230)], T=3, n_draft=[(i * 7) % 4 for i in range(230)], hq=4, hkv=2, S=16),
+    # a CTA works through several lists of units, some of them with nothing to do
+    "lists_of_units": dict(lens=[(29 * i) % 50 for i in range(2600)], T=2, n_draft=[(i * 5) % 3 for i in range(2600)], hq=2, hkv=2, S=16),
+    "lists_of_units_wide": dict(lens=[(29 * i) % 50 for i in range(1700)], T=130, n_draft=[(i * 11) % 131 for i in range(1700)], hq=3, hkv=3,
+                                S=32, mask="chain"),
+    # more selected pages of a KV head than its list kernel holds in registers
+    "selected_thousands": dict(lens=[6405, 100], T=2, n_draft=[2, 1], hq=16, hkv=2, S=16, top_k=300),
+    # more blocks of rows than SMs
+    "row_blocks_beyond_sms": dict(lens=[70, 0], T=700, n_draft=[650, 700], hq=64, hkv=1, S=16, mask="chain"),
+    "long_chunk": dict(lens=[1000], T=2100, n_draft=[2100], hq=8, hkv=2, S=16, mask="chain"),
+}
+
+
+@pytest.mark.parametrize("name", list(MANY))
+def test_many_units_and_rows(name):
+    c = Case(seed=len(name), **MANY[name])
+    c.run()
+    c.check()
+    assert B.swarm_device_status(c.ctx) == 0
+    c.close()
