@@ -336,3 +336,22 @@ def test_moves_count_and_refusals():
         lay.moves(src=[1], dst=[2])
     assert e.value.code == B.ERR_WORKSPACE_TOO_SMALL
     close(lay.ctx)
+
+
+def test_plan_and_moves_of_many_requests():
+    """More requests than a plan's CTA has threads, freed, thinned out and grown inside the pool."""
+    rng, lens, owned = random_layout(91, 700, most=4)
+    lay = Layout(lens, owned, sum(owned) + 300, hkv=1, seed=9)
+    left = np.flatnonzero(rng.random(700) < 0.8)
+    parent = np.full(700, -1)
+    parent[np.sort(rng.permutation(700)[: len(left)])] = left
+    reserve = (rng.random(700) < 0.2).astype(int)
+    keep = (rng.random(lay.n_pool) < 0.9).astype(np.uint8)
+    want = plan_reference(lay.base, lens, parent, reserve, keep, 16)
+    moved = lay.expect(list(zip(want[2], want[3])))
+    lay.plan(parent, reserve, keep, in_place=True)
+    torch.cuda.synchronize()
+    assert lay.new_base.tolist() == want[0] and lay.new_len.tolist() == want[1] and int(lay.n) == len(want[2])
+    lay.moves()
+    assert lay.matches(moved) and B.swarm_device_status(lay.ctx) == 0
+    close(lay.ctx)
