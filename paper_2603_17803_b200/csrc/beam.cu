@@ -252,141 +252,141 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
   bool over = false;
   for (bool careful = false;; careful = true) {
 #pragma unroll
-  for (int i = 0; i < kStages; ++i) fetch(i, i < n_whole);
-  int stage = 0;
-  bool more = false;                                          // this thread has appended since the last ranking
-  for (int at0 = begin, chunk = 0; at0 < stop; at0 += kChunk, ++chunk) {
-    float x[kPer];
-    if (chunk < n_whole) {
-      uint4 raw[kVecs];
-      chunk_of(stage, raw);
+    for (int i = 0; i < kStages; ++i) fetch(i, i < n_whole);
+    int stage = 0;
+    bool more = false;                                          // this thread has appended since the last ranking
+    for (int at0 = begin, chunk = 0; at0 < stop; at0 += kChunk, ++chunk) {
+      float x[kPer];
+      if (chunk < n_whole) {
+        uint4 raw[kVecs];
+        chunk_of(stage, raw);
 #pragma unroll
-      for (int i = 0; i < kVecs; ++i) Element<T>::unpack(raw[i], x + i * kVec);
-      fetch(stage, chunk + kStages < n_whole);
-      if (++stage == kStages) stage = 0;
-    } else {
+        for (int i = 0; i < kVecs; ++i) Element<T>::unpack(raw[i], x + i * kVec);
+        fetch(stage, chunk + kStages < n_whole);
+        if (++stage == kStages) stage = 0;
+      } else {
 #pragma unroll
-      for (int i = 0; i < kVecs; ++i) {
-        const int at = at0 + (i * kBeamThreads + tid) * kVec;
+        for (int i = 0; i < kVecs; ++i) {
+          const int at = at0 + (i * kBeamThreads + tid) * kVec;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) x[i * kVec + e] = at + e < V ? Element<T>::one(first, at + e) : -INFINITY;
+          for (int e = 0; e < kVec; ++e) x[i * kVec + e] = at + e < V ? Element<T>::one(first, at + e) : -INFINITY;
+        }
       }
-    }
-    float best4[4];                                           // of quarters of the thread's logits
+      float best4[4];                                           // of quarters of the thread's logits
 #pragma unroll
-    for (int z = 0; z < 4; ++z) {
-      best4[z] = fmaxf(x[z * kPer / 4], x[z * kPer / 4 + 1]);
+      for (int z = 0; z < 4; ++z) {
+        best4[z] = fmaxf(x[z * kPer / 4], x[z * kPer / 4 + 1]);
 #pragma unroll
-      for (int e = 2; e < kPer / 4; e += 2) best4[z] = max3(best4[z], x[z * kPer / 4 + e], x[z * kPer / 4 + e + 1]);
-    }
-    const float mine = fmaxf(max3(best4[0], best4[1], best4[2]), best4[3]);
-    if (mine > top + kSlack) {                                // (-inf: any finite value)
-      sum *= exp_fast(top - mine);                            // (0 * 2^-inf the first time)
-      top = mine;
-    }
-    const float ref = top == -INFINITY ? 0.f : top;
-    const float part = sum_exp(x, ref);
-    if (part == part) {
-      sum += part;
-    } else {                                                  // NaN among them: never chosen, counted as nothing
+        for (int e = 2; e < kPer / 4; e += 2) best4[z] = max3(best4[z], x[z * kPer / 4 + e], x[z * kPer / 4 + e + 1]);
+      }
+      const float mine = fmaxf(max3(best4[0], best4[1], best4[2]), best4[3]);
+      if (mine > top + kSlack) {                                // (-inf: any finite value)
+        sum *= exp_fast(top - mine);                            // (0 * 2^-inf the first time)
+        top = mine;
+      }
+      const float ref = top == -INFINITY ? 0.f : top;
+      const float part = sum_exp(x, ref);
+      if (part == part) {
+        sum += part;
+      } else {                                                  // NaN among them: never chosen, counted as nothing
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) x[e] = fmaxf(x[e], -INFINITY);
-      sum += sum_exp(x, ref);
-    }
+        for (int e = 0; e < kPer; ++e) x[e] = fmaxf(x[e], -INFINITY);
+        sum += sum_exp(x, ref);
+      }
 
-    // Candidates: logits above the floor.
-    auto token = [&](int e) { return (uint32_t)(at0 + ((e / kVec) * kBeamThreads + tid) * kVec + e % kVec); };
-    if (!careful && chunk > 0) {
-      if (__any_sync(0xFFFFFFFFu, mine > floor_)) {
+      // Candidates: logits above the floor.
+      auto token = [&](int e) { return (uint32_t)(at0 + ((e / kVec) * kBeamThreads + tid) * kVec + e % kVec); };
+      if (!careful && chunk > 0) {
+        if (__any_sync(0xFFFFFFFFu, mine > floor_)) {
+#pragma unroll
+          for (int z = 0; z < 4; ++z) {
+            if (!__any_sync(0xFFFFFFFFu, best4[z] > floor_)) continue;
+#pragma unroll
+            for (int e = z * kPer / 4; e < (z + 1) * kPer / 4; ++e) {
+              if (x[e] > floor_) {
+                const int at = atomicAdd(&s_count, 1);
+                if (at < kRoom) s_cand[at] = make_key(x[e], token(e));
+                else over = true;
+                more = true;
+              }
+            }
+          }
+        }
+        if ((chunk & (chunk + 1)) == 0 || (chunk & 7) == 7) {
+          if (__syncthreads_or(more)) {
+            if (__syncthreads_or(over)) break;
+            rank();
+            __syncthreads();
+            more = false;
+          }
+        }
+        continue;
+      }
+      const int hits = __syncthreads_count(mine > floor_);
+      if (hits == 0) continue;
+      const int held = s_count;
+      __syncthreads();
+      if (held >= (hits > kMany ? keep + 1 : gather)) {         // (many hits: the bound below may bring as many as fit beside n_keep)
+        rank();
+        __syncthreads();
+      }
+      key_t bound = 0;
+      float bound_value = -INFINITY;
+      if (hits > kMany) {
+        const int group = keep > 32 ? 2 : 4, groups = kBeamThreads / group;
+        int where = 0;
+#pragma unroll
+        for (int e = kPer - 1; e >= 0; --e)
+          if (x[e] == mine) where = e;                          // the first of equal ones
+        key_t best = make_key(mine, token(where));
+        for (int o = 1; o < group; o <<= 1) {
+          const key_t other = __shfl_xor_sync(0xFFFFFFFFu, best, o);
+          if (other > best) best = other;
+        }
+        if (tid % group == 0) s_max[tid / group] = best;
+        __syncthreads();
+        if (tid < groups) {
+          const key_t my_key = s_max[tid];
+          int above = 0;
+#pragma unroll 8
+          for (int i = 0; i < groups; i += 2) {
+            const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(s_max + i);
+            above += (two.x > my_key) + (two.y > my_key);
+          }
+          if (above == keep - 1) s_bound = my_key;
+        }
+        __syncthreads();
+        bound = s_bound;
+        bound_value = key_value(bound);
+      }
+      if (__any_sync(0xFFFFFFFFu, mine > floor_ && mine >= bound_value)) {
 #pragma unroll
         for (int z = 0; z < 4; ++z) {
-          if (!__any_sync(0xFFFFFFFFu, best4[z] > floor_)) continue;
+          if (!__any_sync(0xFFFFFFFFu, best4[z] > floor_ && best4[z] >= bound_value)) continue;
 #pragma unroll
           for (int e = z * kPer / 4; e < (z + 1) * kPer / 4; ++e) {
-            if (x[e] > floor_) {
-              const int at = atomicAdd(&s_count, 1);
-              if (at < kRoom) s_cand[at] = make_key(x[e], token(e));
-              else over = true;
-              more = true;
+            if (x[e] > floor_ && x[e] >= bound_value) {
+              const key_t k = make_key(x[e], token(e));
+              if (k >= bound) s_cand[atomicAdd(&s_count, 1)] = k;
             }
           }
         }
       }
-      if ((chunk & (chunk + 1)) == 0 || (chunk & 7) == 7) {
-        if (__syncthreads_or(more)) {
-          if (__syncthreads_or(over)) break;
-          rank();
-          __syncthreads();
-          more = false;
-        }
-      }
-      continue;
-    }
-    const int hits = __syncthreads_count(mine > floor_);
-    if (hits == 0) continue;
-    const int held = s_count;
-    __syncthreads();
-    if (held >= (hits > kMany ? keep + 1 : gather)) {         // (many hits: the bound below may bring as many as fit beside n_keep)
-      rank();
-      __syncthreads();
-    }
-    key_t bound = 0;
-    float bound_value = -INFINITY;
-    if (hits > kMany) {
-      const int group = keep > 32 ? 2 : 4, groups = kBeamThreads / group;
-      int where = 0;
-#pragma unroll
-      for (int e = kPer - 1; e >= 0; --e)
-        if (x[e] == mine) where = e;                          // the first of equal ones
-      key_t best = make_key(mine, token(where));
-      for (int o = 1; o < group; o <<= 1) {
-        const key_t other = __shfl_xor_sync(0xFFFFFFFFu, best, o);
-        if (other > best) best = other;
-      }
-      if (tid % group == 0) s_max[tid / group] = best;
-      __syncthreads();
-      if (tid < groups) {
-        const key_t my_key = s_max[tid];
-        int above = 0;
-#pragma unroll 8
-        for (int i = 0; i < groups; i += 2) {
-          const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(s_max + i);
-          above += (two.x > my_key) + (two.y > my_key);
-        }
-        if (above == keep - 1) s_bound = my_key;
-      }
-      __syncthreads();
-      bound = s_bound;
-      bound_value = key_value(bound);
-    }
-    if (__any_sync(0xFFFFFFFFu, mine > floor_ && mine >= bound_value)) {
-#pragma unroll
-      for (int z = 0; z < 4; ++z) {
-        if (!__any_sync(0xFFFFFFFFu, best4[z] > floor_ && best4[z] >= bound_value)) continue;
-#pragma unroll
-        for (int e = z * kPer / 4; e < (z + 1) * kPer / 4; ++e) {
-          if (x[e] > floor_ && x[e] >= bound_value) {
-            const key_t k = make_key(x[e], token(e));
-            if (k >= bound) s_cand[atomicAdd(&s_count, 1)] = k;
-          }
-        }
+      if (!careful) {                                           // (the first chunk: a floor for the others)
+        __syncthreads();
+        rank();
+        __syncthreads();
       }
     }
-    if (!careful) {                                           // (the first chunk: a floor for the others)
-      __syncthreads();
-      rank();
-      __syncthreads();
-    }
-  }
-  if (!__syncthreads_or(over)) break;
-  // once more, from the start (copies under way would still write to the ring)
-  asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncwarp();
-  over = false;
-  if (tid == 0) s_count = 0;
-  top = floor_ = -INFINITY;
-  sum = 0.f;
-  next = start;
+    if (!__syncthreads_or(over)) break;
+    // once more, from the start (copies under way would still write to the ring)
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+    over = false;
+    if (tid == 0) s_count = 0;
+    top = floor_ = -INFINITY;
+    sum = 0.f;
+    next = start;
   }
   if (s_count > keep) rank();
   __syncthreads();
