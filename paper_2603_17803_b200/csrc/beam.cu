@@ -279,7 +279,7 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
 #pragma unroll
         for (int e = 2; e < kPer / 4; e += 2) best4[z] = max3(best4[z], x[z * kPer / 4 + e], x[z * kPer / 4 + e + 1]);
       }
-      const float mine = fmaxf(max3(best4[0], best4[1], best4[2]), best4[3]);
+      float mine = fmaxf(max3(best4[0], best4[1], best4[2]), best4[3]);
       if (mine > top + kSlack) {                                // (-inf: any finite value)
         sum *= exp_fast(top - mine);                            // (0 * 2^-inf the first time)
         top = mine;
@@ -291,6 +291,7 @@ beam_chunk_kernel(const BeamCall c, int stretches, int span, key_t* __restrict__
       } else {                                                  // NaN among them: never chosen, counted as nothing
 #pragma unroll
         for (int e = 0; e < kPer; ++e) x[e] = fmaxf(x[e], -INFINITY);
+        mine = fmaxf(mine, -INFINITY);                          // (nothing but NaN: its key must not stand above a logit's)
         sum += sum_exp(x, ref);
       }
 

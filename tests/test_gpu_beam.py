@@ -195,3 +195,31 @@ def test_whole_rows_in_a_stretch(order):
         if order != "random":
             x = x.sort(-1, descending=order == "falling").values
         check(x.to(dtype), -torch.rand((330, 2), generator=gen, device=DEV), 33)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("batch", [1, 20])
+@pytest.mark.parametrize("lo,n", [(0, 2200), (0, 3100), (0, 3600), (0, 7000), (4096, 3600), (8192, 7000), (1, 20000)])
+def test_blocks_of_nan_take_nothing_from_the_others(lo, n, batch, dtype):
+    """A shard of the vocabulary that failed: threads with nothing but NaN beside threads with ordinary logits.  The best continuations
+    stand right behind the block, in its chunk; with 1 and 20 prompts a chunk of 16-bit logits has 4096 and 8192 tokens.  Once with
+    logits of both signs, once with log probabilities (all of them negative)."""
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    logits = torch.randn((batch, 3, 20011), generator=gen, device=DEV) * 3
+    logits[:, :, lo + n: lo + n + 5] = torch.tensor([20.0, 24.0, 28.0, 22.0, 26.0], device=DEV)
+    logits[:, :, lo: lo + n] = math.nan
+    score = -torch.rand((batch, 3), generator=gen, device=DEV) * 5
+    for keep in (4, 8, 40, 64):
+        check(logits.to(dtype), score, keep)
+        check((logits - 60).to(dtype), score, keep)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_blocks_of_nan_in_rising_rows(dtype):
+    """Rows that bring more candidates than there is room for and are gone through once more, with blocks of NaN in several chunks."""
+    gen = torch.Generator(device=DEV).manual_seed(29)
+    x = (torch.randn((330, 2, 36865), generator=gen, device=DEV) * 4).sort(-1).values
+    for lo, n in ((0, 3600), (8192, 7000), (20480, 3100), (32768, 3600)):
+        x[:, :, lo: lo + n] = math.nan
+    for keep, below in ((5, 0), (33, 60), (5, 60)):
+        check((x - below).to(dtype), -torch.rand((330, 2), generator=gen, device=DEV), keep)
