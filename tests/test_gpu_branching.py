@@ -557,3 +557,25 @@ def test_counts_that_do_not_fit_are_refused():
             B.swarm_move_pages(lay.ctx, moves, ws)
         assert e.value.code == code
     close(lay.ctx)
+
+
+@pytest.mark.parametrize("length", [2 ** 31 - 1, 2 ** 31 - 15, 2 ** 31 - 16])
+@pytest.mark.parametrize("top_k", [0, 4])
+def test_the_largest_lengths_do_not_fit(length, top_k):
+    """Their pages cannot be counted as (length + S - 1) / S in 32 bits: 2^31 - 16 is the last length that could."""
+    c = Case(lens=[100, 50, 30], T=4, n_draft=[4, 4, 4], hq=8, hkv=2, S=16, seed=2, top_k=top_k)
+    c.ctx_len.copy_(dev([100, length, 30]))
+    c.run()
+    torch.cuda.synchronize()
+    bits = B.swarm_device_status(c.ctx)                         # (no page of a request without pages can be selected)
+    assert bits == (B.DEV_BAD_LENGTH | B.DEV_BAD_PAGE if top_k else B.DEV_BAD_LENGTH)
+    assert bool((c.out[1] == 7.0).all()) and bool((c.lse[1] == 7.0).all())
+    c.n_draft = [4, 0, 4]                                       # the others are what they would be alone
+    c.check()
+    c.close()
+    lay = Layout([20, 40, 5], [2, 4, 1], 8, hkv=1)
+    lay.ctx_len.copy_(dev([20, length, 5]))
+    lay.plan([0, 1, 2])
+    assert B.swarm_device_status(lay.ctx) == B.DEV_BAD_LENGTH and int(lay.n) == -1
+    assert lay.new_base.tolist() == lay.base and lay.new_len.tolist() == [20, length, 5]
+    close(lay.ctx)
