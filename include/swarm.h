@@ -485,8 +485,8 @@ int32_t swarm_tree_attn(swarm_ctx* ctx, const swarm_inputs* inputs, const swarm_
  * may be inputs->ctx_len itself).  With ksum the summaries of the pages written to are brought up to date: they must
  * describe the tokens that those pages held, as swarm_build_summaries or earlier calls left them.  For decoded tokens, for
  * the accepted path of a drafted tree (new->path; a token may be named twice) and for prompts.
- * A request whose new length does not fit the pages it owns (or with n_new out of range) sets SWARM_DEV_BAD_LENGTH and
- * is left as it was.  A path entry outside 0..T-1 sets SWARM_DEV_BAD_TOKEN; its rows are written as zeros.
+ * A request whose new length does not fit the pages it owns, whose pages lie outside the pool, or with n_new out of range
+ * sets SWARM_DEV_BAD_LENGTH and is left as it was.  A path entry outside 0..T-1 sets SWARM_DEV_BAD_TOKEN; its rows are written as zeros.
  * page2cluster entries of pages that are written to for the first time are the caller's.  With a tail stream, swarm_tail_join
  * comes first; with the index prefetch on, at least one operation between this call and the step.
  * Reads inputs->page_base, ctx_len.  kv_pool as in swarm_inputs, ksum bf16 [n_pool_pages][Hkv][2][d] or NULL. */

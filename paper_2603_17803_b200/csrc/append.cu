@@ -29,8 +29,9 @@ append_kernel(const Geometry geo, const AppendCall c, int ctas, unsigned* __rest
   const int b = blockIdx.x / ctas, cta = blockIdx.x - b * ctas, lane = threadIdx.x & 31;
   const int S = geo.S, Hkv = geo.Hkv;
   const int len = c.ctx_len[b], n = c.n_new[b];
-  const long long base = c.page_base[b], room = (c.page_base[b + 1] - base) * S;
-  const bool bad = len < 0 || n < 0 || n > c.n_places || (long long)len + n > room;
+  const long long base = c.page_base[b], owned = c.page_base[b + 1] - base;
+  // (a range that is not inside the pool would be written to all the same)
+  const bool bad = len < 0 || n < 0 || n > c.n_places || (long long)len + n > owned * S || base < 0 || base + owned > geo.n_pool_pages;
   const bool in_place = c.ctx_len_out == c.ctx_len;
   if (in_place) __syncthreads();                             // every thread has its length before this CTA counts as having read it
   if (threadIdx.x == 0) {

@@ -355,3 +355,38 @@ def test_plan_and_moves_of_many_requests():
     lay.moves()
     assert lay.matches(moved) and B.swarm_device_status(lay.ctx) == 0
     close(lay.ctx)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("table", [[0, 2, 6, 12], [0, 2, 6, 1 << 40], [-3, -1, 1, 6], [0, 5, 9, 13]])
+def test_append_writes_nothing_outside_the_pool(table, in_place):
+    """Page tables that name pages behind the pool (8 pages of it) or in front of it; the tensors go on on both sides."""
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    hkv, S, n_pool, edge = 2, 16, 8, 8
+    whole = torch.randn((edge + n_pool + edge, hkv, 2, S, D), generator=gen, device=DEV).to(torch.bfloat16)
+    sums = torch.randn((edge + n_pool + edge, hkv, 2, D), generator=gen, device=DEV).to(torch.bfloat16)
+    k, v = (torch.randn((3, 8, hkv, D), generator=gen, device=DEV).to(torch.bfloat16) for _ in range(2))
+    shape, ctx, ws = handle(3, hkv, S, n_pool, 8)
+    base, lens, n_new = dev(table, torch.int64), dev([10, 20, 3]), dev([8, 5, 7])
+    want, want_sums, want_len = whole.clone(), sums.clone(), [10, 20, 3]
+    for b, (n, m) in enumerate(zip([10, 20, 3], [8, 5, 7])):
+        if table[b] < 0 or table[b + 1] > n_pool:
+            continue
+        want_len[b] = n + m
+        for i in range(m):
+            for z, x in enumerate((k, v)):
+                want[edge + table[b] + (n + i) // S, :, z, (n + i) % S] = x[b, i]
+        for p in range(n // S, (n + m - 1) // S + 1):
+            at, lo = edge + table[b] + p, max(n - p * S, 0)
+            K = want[at, :, 0, lo: min(S, n + m - p * S)].float()
+            low, high = K.amin(1), K.amax(1)
+            if lo:                                              # the page held tokens: their summary takes part
+                low, high = torch.minimum(low, sums[at, :, 0].float()), torch.maximum(high, sums[at, :, 1].float())
+            want_sums[at, :, 0], want_sums[at, :, 1] = low, high
+    out = lens if in_place else torch.zeros_like(lens)
+    B.swarm_append_tokens(ctx, B.make_inputs(page_base=base, ctx_len=lens), B.make_new_tokens(k=k, v=v, n_new=n_new),
+                          whole[edge: edge + n_pool], sums[edge: edge + n_pool], out)
+    torch.cuda.synchronize()
+    assert same(whole, want) and same(sums, want_sums) and out.tolist() == want_len
+    assert B.swarm_device_status(ctx) == B.DEV_BAD_LENGTH
+    close(ctx)
