@@ -470,8 +470,9 @@ int32_t swarm_build_clusters(const float* dist, int32_t n_entries, float tau, vo
  * writes them (a page listed twice counts once; ids outside the request set SWARM_DEV_BAD_PAGE and are skipped); NULL:
  * all pages.  A row that sees no token gives out = 0, lse = -inf.  Rows t >= n_draft[b] of out and lse are left as
  * they were.  out is bf16 [B][T][Hq][d] (the weights enter the product with V as bf16), lse f32 [B][T][Hq].
- * A context length that does not fit the request's pages sets SWARM_DEV_BAD_LENGTH and the request's rows are left as they
- * were; n_draft outside 0..T sets it too and is clamped.
+ * A context length that does not fit the request's pages (with a selection: or max_pages_per_req, which bounds what swarm_select
+ * selects from) sets SWARM_DEV_BAD_LENGTH and the request's rows are left as they were; n_draft outside 0..T sets it too and
+ * is clamped.
  * Reads inputs->kv_pool, page_base, ctx_len.  workspace: swarm_tree_attn_workspace_bytes(shape, T) bytes of device
  * memory (256-byte aligned, contents irrelevant), used by one call at a time; < 0: minus an error code.
  * SWARM_ERR_UNSUPPORTED: n_pool_pages >= 2^31 or more than 128 query heads per KV head; with a selection, more than 32 query
@@ -485,8 +486,8 @@ int32_t swarm_tree_attn(swarm_ctx* ctx, const swarm_inputs* inputs, const swarm_
  * may be inputs->ctx_len itself).  With ksum the summaries of the pages written to are brought up to date: they must
  * describe the tokens that those pages held, as swarm_build_summaries or earlier calls left them.  For decoded tokens, for
  * the accepted path of a drafted tree (new->path; a token may be named twice) and for prompts.
- * A request whose new length does not fit the pages it owns, whose pages lie outside the pool, or with n_new out of range
- * sets SWARM_DEV_BAD_LENGTH and is left as it was.  A path entry outside 0..T-1 sets SWARM_DEV_BAD_TOKEN; its rows are written as zeros.
+ * A request whose new length does not fit the pages it owns or max_pages_per_req (no step could use it then), whose pages lie
+ * outside the pool, or with n_new out of range sets SWARM_DEV_BAD_LENGTH and is left as it was.  A path entry outside 0..T-1 sets SWARM_DEV_BAD_TOKEN; its rows are written as zeros.
  * page2cluster entries of pages that are written to for the first time are the caller's.  With a tail stream, swarm_tail_join
  * comes first; with the index prefetch on, at least one operation between this call and the step.
  * Reads inputs->page_base, ctx_len.  kv_pool as in swarm_inputs, ksum bf16 [n_pool_pages][Hkv][2][d] or NULL. */

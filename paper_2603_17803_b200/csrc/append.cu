@@ -31,7 +31,8 @@ append_kernel(const Geometry geo, const AppendCall c, int ctas, unsigned* __rest
   const int len = c.ctx_len[b], n = c.n_new[b];
   const long long base = c.page_base[b], owned = c.page_base[b + 1] - base;
   // (a range that is not inside the pool would be written to all the same)
-  const bool bad = len < 0 || n < 0 || n > c.n_places || (long long)len + n > owned * S || base < 0 || base + owned > geo.n_pool_pages;
+  const bool bad = len < 0 || n < 0 || n > c.n_places || (long long)len + n > min(owned, (long long)geo.Pmax) * S || base < 0 ||
+                   base + owned > geo.n_pool_pages;
   const bool in_place = c.ctx_len_out == c.ctx_len;
   if (in_place) __syncthreads();                             // every thread has its length before this CTA counts as having read it
   if (threadIdx.x == 0) {

@@ -255,6 +255,11 @@ struct TreeArgs {
   uint32_t* status;
 };
 
+// A length fits the request's pages, and, where pages are selected, the lists of at most Pmax pages that the selection makes.
+__device__ __forceinline__ bool length_fits(const TreeArgs& a, int len, long long owned) {
+  const int P = pages_of(len, a.geo.S);
+  return len >= 0 && P <= owned && (a.list == nullptr || P <= a.geo.Pmax);
+}
 // Context tokens (those of the selected pages, if there is a selection), drafted tokens and first pool page of a unit; no drafted
 // tokens where the request's length does not fit its pages.
 __device__ __forceinline__ void unit_lengths(const TreeArgs& a, int u, int& ctx, int& nd, int& base, bool& bad) {
@@ -265,7 +270,7 @@ __device__ __forceinline__ void unit_lengths(const TreeArgs& a, int u, int& ctx,
   nd = a.n_draft[b];
   bad = nd < 0 || nd > a.T;
   nd = max(0, min(nd, a.T));
-  if (len < 0 || pages_of(len, a.geo.S) > owned) {
+  if (!length_fits(a, len, owned)) {
     bad = true;
     nd = 0;
   }
@@ -874,7 +879,7 @@ tree_merge_kernel(const TreeArgs a, int groups, int tiles) {
   // has not waited for anything yet)
   const int len = __ldcg(a.ctx_len + b);
   const long long owned = __ldcg(a.page_base + b + 1) - __ldcg(a.page_base + b);
-  const int nd = len < 0 || pages_of(len, a.geo.S) > owned ? 0 : max(0, min(__ldcg(a.n_draft + b), a.T));
+  const int nd = !length_fits(a, len, owned) ? 0 : max(0, min(__ldcg(a.n_draft + b), a.T));
   pdl_wait();
   const int first = a.unit_first[u], last = a.unit_last[u];  // (not written where nd is 0)
   pdl_launch_dependents();
@@ -984,7 +989,7 @@ tree_list_kernel(const TreeArgs a, const int32_t* __restrict__ sel, const int32_
   __syncthreads();
   const int S = a.geo.S, len = a.ctx_len[b];
   const long long owned = a.page_base[b + 1] - a.page_base[b];
-  const int P = len < 0 || pages_of(len, S) > owned ? 0 : min(pages_of(len, S), a.geo.Pmax);
+  const int P = length_fits(a, len, owned) ? pages_of(len, S) : 0;
   // every selected page of the group's heads: kHold entries of a thread at a time, all loads ahead of their uses (4 heads with 256
   // pages: 6.1 us, one after the other 8.3); the first ones are kept for the second look
   const int k = a.geo.k, entries = a.geo.g * k;
@@ -1174,11 +1179,11 @@ cudaError_t launch_tree_attn(const Geometry& geo, const TreeCall& c, void* works
   if (c.sel != nullptr) {
     int2* list = reinterpret_cast<int2*>(ws + lay.list);
     int32_t* tokens = reinterpret_cast<int32_t*>(ws + lay.list_tokens);
+    a.list = list;
+    a.list_tokens = tokens;
     e = launch_pdl(tree_list_kernel, dim3((unsigned)(geo.B * geo.Hkv)), dim3(256), (size_t)((geo.Pmax + 31) / 32) * 8, st, true, a, c.sel,
                    c.n_sel, list, tokens);
     if (e != cudaSuccess) return e;
-    a.list = list;
-    a.list_tokens = tokens;
   }
   const int tiles = row_tiles_of(geo, c.T);
   const bool wide = tiles > 1;

@@ -579,3 +579,24 @@ def test_the_largest_lengths_do_not_fit(length, top_k):
     assert B.swarm_device_status(lay.ctx) == B.DEV_BAD_LENGTH and int(lay.n) == -1
     assert lay.new_base.tolist() == lay.base and lay.new_len.tolist() == [20, length, 5]
     close(lay.ctx)
+
+
+def test_selections_of_requests_with_more_pages_than_the_ctx_has():
+    """Request 0 has 19 pages, in a ctx for 7: nothing can have been selected from it.  Over all pages it is attended all the same."""
+    c = Case(lens=[300, 100], T=3, n_draft=[3, 3], hq=4, hkv=2, S=16, seed=3, top_k=5)
+    B.swarm_destroy(c.ctx)
+    c.shape = B.make_shape(batch=2, n_q_heads=4, n_kv_heads=2, page_size=16, top_k=5, n_queues=1, max_pages_per_req=7,
+                           max_clusters_total=1, n_pool_pages=c.pool.shape[0])
+    c.ctx = B.swarm_create(c.shape)
+    B.swarm_set_workspace(c.ctx, c.ctx_ws)
+    c.n_sel[0] = 0
+    c.run()
+    assert B.swarm_device_status(c.ctx) == B.DEV_BAD_LENGTH
+    c.n_draft = [0, 3]
+    c.check()
+    c.sel = c.n_sel = None
+    c.n_draft = [3, 3]
+    c.run()
+    assert B.swarm_device_status(c.ctx) == 0
+    c.check()
+    c.close()

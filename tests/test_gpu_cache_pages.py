@@ -390,3 +390,19 @@ def test_append_writes_nothing_outside_the_pool(table, in_place):
     assert same(whole, want) and same(sums, want_sums) and out.tolist() == want_len
     assert B.swarm_device_status(ctx) == B.DEV_BAD_LENGTH
     close(ctx)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_append_stops_at_the_pages_that_a_step_can_use(in_place):
+    """Requests of 4 pages in a ctx for 2: what fits 2 pages is written, what does not leaves the request as it was."""
+    c = append_case(lens=[30, 30, 0, 32], owned=[4, 4, 4, 4], n_new=[2, 3, 33, 0], T=40, hkv=2, S=16, path=None, seed=6)
+    B.swarm_destroy(c["ctx"])
+    shape, ctx, ws = handle(4, 2, 16, 18, 2)
+    before, sums, lens = c["pool"].clone(), c["ksum"].clone(), c["t"]["ctx_len"]
+    out = lens if in_place else torch.full_like(lens, -5)
+    B.swarm_append_tokens(ctx, c["inputs"], c["tokens"], c["pool"], c["ksum"], out)
+    assert B.swarm_device_status(ctx) == B.DEV_BAD_LENGTH
+    assert out.tolist() == [32, 30, 0, 32]
+    assert same(c["pool"][:4], c["want"][0][:4]) and torch.equal(c["ksum"][:4].float(), c["want"][1][:4].float())
+    assert same(c["pool"][4:], before[4:]) and same(c["ksum"][4:], sums[4:])
+    close(ctx)
