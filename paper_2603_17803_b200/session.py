@@ -30,12 +30,15 @@ class StepOutputs:
 
 
 class Session:
-    """One ctx bound to one resident KV pool (``workload`` tensors must live on a CUDA device)."""
+    """One ctx bound to one resident KV pool (``workload`` tensors must live on a CUDA device).
+
+    ``max_pages_per_req``: the pages that a request may grow to by append(); at least those of the workload's longest context, which
+    is all there is room for by default."""
 
     def __init__(self, workload, *, flags: int = 0, keep_scores: bool = False, keep_gathered: bool = False,
                  ksum: Optional[torch.Tensor] = None, local_window_pages: int = 0,
                  max_clusters_total: Optional[int] = None, scorer: int = B.SCORER_AUTO, tail_stream=None,
-                 index_prefetch: bool = False):
+                 index_prefetch: bool = False, max_pages_per_req: Optional[int] = None):
         cfg = workload.cfg
         self.cfg = cfg
         self.w = workload
@@ -43,7 +46,7 @@ class Session:
         if dev.type != "cuda":
             raise ValueError("Session needs the workload on a CUDA device")
         self.device = dev
-        self.Pmax = cfg.max_pages()
+        self.Pmax = max(cfg.max_pages(), max_pages_per_req or 0)
         self.shape = B.make_shape(batch=cfg.batch, n_q_heads=cfg.n_q_heads, n_kv_heads=cfg.n_kv_heads,
                                   page_size=cfg.page_size, top_k=cfg.top_k, n_queues=cfg.n_queues,
                                   max_pages_per_req=self.Pmax, max_clusters_total=max(1, workload.n_clusters, max_clusters_total or 0),
@@ -235,7 +238,8 @@ class Session:
     def append(self, k, v, n_new, path=None, stream=None) -> None:
         """swarm_append_tokens into the session's pool: the tokens (k / v [B, T, Hkv, d], all or the accepted ``path``), the
         summaries of the pages they reach and the workload's context lengths, all in place.  The page2cluster entries of
-        pages that are reached for the first time are the caller's."""
+        pages that are reached for the first time are the caller's.  A request that would pass the pages it owns or the session's
+        max_pages_per_req stays as it was and shows in status()."""
         cfg = self.cfg
         self._about_to_write(stream)
         if k.dim() != 4 or tuple(k.shape) != (cfg.batch, k.shape[1], cfg.n_kv_heads, cfg.head_dim):

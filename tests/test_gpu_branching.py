@@ -600,3 +600,56 @@ def test_selections_of_requests_with_more_pages_than_the_ctx_has():
     assert B.swarm_device_status(c.ctx) == 0
     c.check()
     c.close()
+
+
+@pytest.mark.parametrize("S", [16, 32])
+def test_a_request_grows_past_its_configured_length(S):
+    """Pages of one request are dropped, another gets them as spare ones and grows past the longest context that the workload began
+    with: its steps and its trees are then those of a new session over the same tokens.  Without room in the session it stays as
+    it was."""
+    cfg = small(batch=2, ctx_len=S * 60 + 7, page_size=S)
+    P = cfg.max_pages()
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    T, more = 5 * S, [4 * S + 3, S // 2]
+    k, v = (torch.randn((2, T, cfg.n_kv_heads, 128), generator=gen, device=DEV).to(torch.bfloat16) for _ in range(2))
+    t = 6
+    drafts = [torch.randn((2, t, h, 128), generator=gen, device=DEV).to(torch.bfloat16) for h in (cfg.n_q_heads, cfg.n_kv_heads, cfg.n_kv_heads)]
+    for room in (None, P + 6):
+        w = W.generate(cfg, seed=41, device=DEV)
+        lens, base = w.ctx_len.tolist(), w.page_base.tolist()
+        keep = torch.ones(w.n_pool_pages, dtype=torch.uint8, device=DEV)
+        keep[base[1]: base[1] + 6] = 0
+        s = Session(w, max_pages_per_req=room)
+        s.compact(dev([0, 1]), reserve=dev([6, 0]), keep=keep)
+        assert s.status() == 0
+        at = int(w.page_base[0]) + P
+        w.page2cluster[at: at + 6] = 0
+        s.append(k, v, dev(more))
+        if room is None:                                        # request 1 has lost pages, and grows inside its last one
+            assert s.status() == B.DEV_BAD_LENGTH
+            assert w.ctx_len.tolist() == [lens[0], lens[1] - 6 * S + more[1]]
+            s.close()
+            continue
+        assert s.status() == 0 and w.ctx_len.tolist() == [lens[0] + more[0], lens[1] - 6 * S + more[1]]
+        kept = rows_of(w, 0, lens[0], lens[0] + more[0])
+        assert same(kept[0], k[0, : more[0]]) and same(kept[1], v[0, : more[0]])
+        fresh = Session(w, max_pages_per_req=room)
+        for x in (s, fresh):
+            x.step()
+        torch.cuda.synchronize()
+        last = -(-(lens[0] + more[0]) // S) - 1
+        assert int(s.o.n_sel[0].min()) == cfg.top_k and last >= P
+        for f in ("sel", "n_sel", "out", "lse", "n_uniq", "queue_load"):
+            assert same(getattr(s.o, f), getattr(fresh.o, f)), f
+        for selected in (True, False):
+            got, want = (x.tree_attn(*drafts, dev([t, t]), selected=selected) for x in (s, fresh))
+            assert same(got[0], want[0]) and same(got[1], want[1])
+        # the pages beyond the first length are attended: a query that points at the last one finds it
+        q = w.q.clone()
+        q[0] = (kept[0][-1].float() * 4).repeat_interleave(cfg.n_q_heads // cfg.n_kv_heads, 0).to(torch.bfloat16)
+        s.set_query(q)
+        s.select()
+        assert bool((s.o.sel[0] == last).any(-1).all())
+        assert s.status() == 0 and fresh.status() == 0
+        s.close()
+        fresh.close()
