@@ -241,6 +241,8 @@ class Session:
         pages that are reached for the first time are the caller's.  A request that would pass the pages it owns or the session's
         max_pages_per_req stays as it was and shows in status()."""
         cfg = self.cfg
+        if hasattr(self, "medoid_index"):
+            raise ValueError("the medoid index holds summaries and lists of the pages there were: append before enable_medoid_index()")
         self._about_to_write(stream)
         if k.dim() != 4 or tuple(k.shape) != (cfg.batch, k.shape[1], cfg.n_kv_heads, cfg.head_dim):
             raise ValueError(f"k must have shape {(cfg.batch, 'T', cfg.n_kv_heads, cfg.head_dim)}, not {tuple(k.shape)}")

@@ -653,3 +653,19 @@ def test_a_request_grows_past_its_configured_length(S):
         assert s.status() == 0 and fresh.status() == 0
         s.close()
         fresh.close()
+
+
+def test_nothing_is_appended_under_a_medoid_index():
+    """The index copies the summaries of the medoids' pages and lists the clusters' pages: both would be stale."""
+    cfg = small(ctx_len=16 * 60 + 7)
+    w = W.generate(cfg, seed=14, device=DEV)
+    s = Session(w)
+    kv = torch.zeros((3, 1, cfg.n_kv_heads, 128), dtype=torch.bfloat16, device=DEV)
+    s.append(kv, kv, dev([1, 1, 1]))
+    s.enable_medoid_index(4)
+    pool, ksum, lens = w.kv_pool.clone(), s.ksum.clone(), w.ctx_len.clone()
+    with pytest.raises(ValueError, match="medoid"):
+        s.append(kv, kv, dev([1, 1, 1]))
+    assert s.status() == 0
+    assert same(w.kv_pool, pool) and same(s.ksum, ksum) and torch.equal(w.ctx_len, lens)
+    s.close()
