@@ -518,7 +518,7 @@ int32_t swarm_plan_pages(swarm_ctx* ctx, const swarm_page_plan* plan, void* stre
  * one call at a time; < 0: minus an error code.  SWARM_ERR_UNSUPPORTED: n_pool_pages or max_moves >= 2^30, or more than about 2^31
  * blocks of 32 KB in max_moves pages.
  * page2cluster holds ids local to a request and is moved as it is: where requests change places, cluster_base and the
- * tables it points into are the caller's to permute.  With a tail stream, swarm_tail_join comes before moves inside the pool. */
+ * tables it points into are the caller's to permute, those of an attached cache state (swarm_set_cache) among them.  With a tail stream, swarm_tail_join comes before moves inside the pool. */
 int64_t swarm_move_pages_workspace_bytes(const swarm_shape* shape);
 int32_t swarm_move_pages(swarm_ctx* ctx, const swarm_page_moves* moves, void* workspace, int64_t workspace_bytes, void* stream);
 

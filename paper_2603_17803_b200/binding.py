@@ -158,8 +158,13 @@ def swarm_workspace_bytes(shape: swarm_shape) -> int:
     return n
 
 
-def swarm_create(shape: swarm_shape) -> ctypes.c_void_p:
-    ctx = ctypes.c_void_p()
+class swarm_ctx(ctypes.c_void_p):
+    """A ctx's handle, and what was set by way of this module: ``has_cache``, a cache state is attached (swarm_set_cache)."""
+    has_cache = False
+
+
+def swarm_create(shape: swarm_shape) -> swarm_ctx:
+    ctx = swarm_ctx()
     _check(load_library().swarm_create(ctypes.byref(shape), ctypes.byref(ctx)), "swarm_create")
     return ctx
 
@@ -212,10 +217,14 @@ def swarm_set_cache(ctx, *, resident=None, freq=None, score=None, n_hit=None, t_
     when ``resident`` is None.  The caller keeps the tensors alive while they are attached."""
     if resident is None:
         _check(load_library().swarm_set_cache(ctx, None), "swarm_set_cache", ctx)
+        if isinstance(ctx, swarm_ctx):
+            ctx.has_cache = False
         return
     c = swarm_cache(_ptr(resident, "resident"), _ptr(freq, "freq"), _ptr(score, "score"), _ptr(n_hit, "n_hit"),
                     float(t_base), float(t_transfer))
     _check(load_library().swarm_set_cache(ctx, ctypes.byref(c)), "swarm_set_cache", ctx)
+    if isinstance(ctx, swarm_ctx):
+        ctx.has_cache = True
 
 
 def swarm_cache_admit_workspace_bytes(n_clusters: int) -> int:

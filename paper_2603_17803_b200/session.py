@@ -258,6 +258,8 @@ class Session:
         dev, n_pool = self.device, self.w.n_pool_pages
         if hasattr(self, "medoid_index"):
             raise ValueError("the medoid index lists pages by number: compact before enable_medoid_index()")
+        if getattr(self.ctx, "has_cache", False):
+            raise ValueError("the cache state is indexed by global cluster ids, which change: detach it (swarm_set_cache) to compact")
         self._about_to_write(stream)
         if getattr(self, "_pages", None) is None:
             i32 = dict(dtype=torch.int32, device=dev)

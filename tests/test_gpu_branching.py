@@ -669,3 +669,22 @@ def test_nothing_is_appended_under_a_medoid_index():
     assert s.status() == 0
     assert same(w.kv_pool, pool) and same(s.ksum, ksum) and torch.equal(w.ctx_len, lens)
     s.close()
+
+
+def test_nothing_is_compacted_under_a_cache_state():
+    """Its arrays are indexed by global cluster ids, which a compaction changes."""
+    cfg = small(ctx_len=16 * 60 + 7)
+    w = W.generate(cfg, seed=15, device=DEV)
+    s = Session(w)
+    n = w.n_clusters + 16
+    resident, freq = torch.zeros(n, dtype=torch.uint8, device=DEV), torch.zeros(n, dtype=torch.int32, device=DEV)
+    B.swarm_set_cache(s.ctx, resident=resident, freq=freq)
+    tables = [x.clone() for x in (w.kv_pool, w.page_base, w.ctx_len, w.cluster_base, w.page2cluster)]
+    with pytest.raises(ValueError, match="cache state"):
+        s.compact(dev([1, -1, 2]))
+    assert s.status() == 0
+    assert all(same(a, b) for a, b in zip((w.kv_pool, w.page_base, w.ctx_len, w.cluster_base, w.page2cluster), tables))
+    B.swarm_set_cache(s.ctx)
+    s.compact(dev([1, -1, 2]))
+    assert s.status() == 0 and w.ctx_len.tolist()[1] == 0
+    s.close()
