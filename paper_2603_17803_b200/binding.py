@@ -90,6 +90,15 @@ def load_library() -> ctypes.CDLL:
         lib.swarm_beam_select_workspace_bytes.restype = ctypes.c_int64
         v, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
         lib.swarm_build_clusters.argtypes = [v, i32, ctypes.c_float, v, i64, v, v, v, i64, v, v, v, v]
+        # Calls of a few microseconds once more, by the types of their arguments: structs and addresses are passed as they are, which
+        # pays for a part of the checks of the tensors' sizes (an append's host time 4.4 us without checks, 4.6 with them).
+        p = ctypes.POINTER
+        for name, types in (("tree_attn", [v, p(swarm_inputs), p(swarm_tree), v, v, v, i64, v, v, v]),
+                            ("append_tokens", [v, p(swarm_inputs), p(swarm_new_tokens), v, v, v, v]),
+                            ("plan_pages", [v, p(swarm_page_plan), v]), ("move_pages", [v, p(swarm_page_moves), v, i64, v])):
+            call = lib["swarm_" + name]
+            call.restype, call.argtypes = ctypes.c_int32, types
+            setattr(lib, name, call)
         _lib = lib
     return _lib
 
@@ -104,10 +113,14 @@ def _ptr(t: Optional[torch.Tensor], name: str = "tensor", device_check: bool = T
     return ctypes.c_void_p(t.data_ptr())
 
 
-def _stream(stream) -> ctypes.c_void_p:
+def _raw_stream(stream) -> int:
     if stream is None:      # (building torch's stream object costs as much as a launch: 3.6 against 0.3 us)
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
-    return ctypes.c_void_p(stream.cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
+
+
+def _stream(stream) -> ctypes.c_void_p:
+    return ctypes.c_void_p(_raw_stream(stream))
 
 
 def _check(rc: int, what: str, ctx=None):
@@ -159,13 +172,28 @@ def swarm_workspace_bytes(shape: swarm_shape) -> int:
 
 
 class swarm_ctx(ctypes.c_void_p):
-    """A ctx's handle, and what was set by way of this module: ``has_cache``, a cache state is attached (swarm_set_cache)."""
+    """A ctx's handle, with the sizes that tensors used with it have to have (0 and None: not known), and ``has_cache``: a cache
+    state is attached (swarm_set_cache)."""
+    batch = n_rows = sel_elems = n_pool_pages = sum_elems = pool_elems = 0
+    made_for = made_for_tokens = None
     has_cache = False
+
+
+def _bare(ctx) -> swarm_ctx:
+    """A handle that does not come from swarm_create."""
+    return swarm_ctx(getattr(ctx, "value", ctx))
 
 
 def swarm_create(shape: swarm_shape) -> swarm_ctx:
     ctx = swarm_ctx()
     _check(load_library().swarm_create(ctypes.byref(shape), ctypes.byref(ctx)), "swarm_create")
+    ctx.batch, ctx.n_pool_pages = shape.batch, shape.n_pool_pages
+    ctx.made_for = (shape.batch, shape.n_q_heads, shape.n_kv_heads)
+    ctx.made_for_tokens = (shape.batch, shape.n_kv_heads)
+    ctx.n_rows = shape.batch * shape.n_q_heads
+    ctx.sel_elems = ctx.n_rows * shape.top_k
+    ctx.sum_elems = shape.n_pool_pages * shape.n_kv_heads * 2 * shape.head_dim
+    ctx.pool_elems = ctx.sum_elems * shape.page_size
     return ctx
 
 
@@ -435,7 +463,26 @@ def _step_host_fn():
     return _STEP_HOST_FN
 
 
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+def _holds(t: torch.Tensor, name: str, dtype, n: int) -> int:
+    """Address of a CUDA tensor of n elements of the type or more, in whatever shape."""
+    if t.dtype is dtype and t.numel() >= n and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    if t.is_cuda and t.is_contiguous():
+        raise ValueError(f"{name} must be a {dtype} tensor of at least {n} elements, not {t.dtype} {tuple(t.shape)}")
+    raise ValueError(f"{name} must be a contiguous CUDA tensor")
+
+
+def _other_ctx(what: str, made_for, has) -> None:
+    if made_for and has:                                    # (a struct or a handle made elsewhere says nothing about sizes)
+        raise ValueError(f"{what} made for {made_for}, the ctx is for {has}")
+
+
 class swarm_tree(ctypes.Structure):
+    made_for = None                                         # (batch, query heads, KV heads) of its tensors
+
     _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "n_draft", "mask")] + \
                [("max_draft", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
@@ -459,7 +506,9 @@ def make_tree(*, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_draft: tor
     _expect(n_draft, "n_draft", torch.int32, (batch,))
     if mask is not None:
         _expect(mask, "mask", torch.int32, (batch, T, -(-T // 32)))
-    return swarm_tree(_ptr(q, "q"), _ptr(k, "k"), _ptr(v, "v"), _ptr(n_draft, "n_draft"), _ptr(mask, "mask"), T, 0)
+    tree = swarm_tree(_ptr(q, "q"), _ptr(k, "k"), _ptr(v, "v"), _ptr(n_draft, "n_draft"), _ptr(mask, "mask"), T, 0)
+    tree.made_for = (batch, q.shape[2], k.shape[2])
+    return tree
 
 
 def swarm_tree_attn_workspace_bytes(shape: swarm_shape, max_draft: int) -> int:
@@ -473,28 +522,39 @@ def swarm_tree_attn(ctx, inputs: swarm_inputs, tree: swarm_tree, sel: Optional[t
                     workspace: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, stream=None) -> None:
     """Attention of the drafted tokens over the context (all pages, or those selected per head) and over one another;
     out bf16 [B, T, Hq, 128], lse float32 [B, T, Hq]."""
-    if out.dtype != torch.bfloat16 or lse.dtype != torch.float32:
-        raise ValueError("out must be bfloat16 and lse float32")
-    rc = load_library().swarm_tree_attn(ctx, ctypes.byref(inputs), ctypes.byref(tree), _ptr(sel, "sel"), _ptr(n_sel, "n_sel"),
-                                        _ptr(workspace, "workspace"),
-                                        ctypes.c_int64(workspace.numel() * workspace.element_size()), _ptr(out, "out"),
-                                        _ptr(lse, "lse"), _stream(stream))
+    if type(ctx) is not swarm_ctx:
+        ctx = _bare(ctx)
+    if tree.made_for != ctx.made_for:
+        _other_ctx("drafted tokens", tree.made_for, ctx.made_for)
+    rows = ctx.n_rows * tree.max_draft
+    if sel is not None and n_sel is not None:               # (one without the other is refused below)
+        sel, n_sel = _holds(sel, "sel", _I32, ctx.sel_elems), _holds(n_sel, "n_sel", _I32, ctx.n_rows)
+    else:
+        sel, n_sel = _ptr(sel, "sel"), _ptr(n_sel, "n_sel")
+    rc = load_library().tree_attn(ctx, inputs, tree, sel, n_sel, _ptr(workspace, "workspace"), workspace.nbytes,
+                                  _holds(out, "out", _BF16, rows * 128), _holds(lse, "lse", _F32, rows), _raw_stream(stream))
     if rc != OK:
         _check(rc, "swarm_tree_attn", ctx)
 
 
 class swarm_new_tokens(ctypes.Structure):
+    made_for = None                                         # (batch, KV heads) of its tensors
+
     _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "n_new", "path")] + \
                [("max_new", ctypes.c_int32), ("max_path", ctypes.c_int32)]
 
 
 class swarm_page_plan(ctypes.Structure):
+    made_for = n_keep = None                                # requests; entries of keep
+
     _fields_ = [(n, ctypes.c_void_p) for n in ("page_base", "ctx_len", "parent", "reserve", "keep", "new_page_base",
                                                "new_ctx_len", "src", "dst", "n_moves")] + \
                [("max_moves", ctypes.c_int32), ("in_place", ctypes.c_int32)]
 
 
 class swarm_page_moves(ctypes.Structure):
+    made_for = None                                         # elements of (pool, summaries, page2cluster), None where there are none
+
     _fields_ = [(n, ctypes.c_void_p) for n in ("src", "dst", "n_moves", "from_pool", "to_pool", "from_ksum", "to_ksum",
                                                "from_page2cluster", "to_page2cluster")] + \
                [("max_moves", ctypes.c_int32), ("reserved", ctypes.c_int32)]
@@ -512,16 +572,23 @@ def make_new_tokens(*, k: torch.Tensor, v: torch.Tensor, n_new: torch.Tensor,
     _expect(n_new, "n_new", torch.int32, (batch,))
     if path is not None:
         _expect(path, "path", torch.int32, (batch, path.shape[-1]))
-    return swarm_new_tokens(_ptr(k, "k"), _ptr(v, "v"), _ptr(n_new, "n_new"), _ptr(path, "path"), T,
-                            0 if path is None else path.shape[1])
+    tokens = swarm_new_tokens(_ptr(k, "k"), _ptr(v, "v"), _ptr(n_new, "n_new"), _ptr(path, "path"), T,
+                              0 if path is None else path.shape[1])
+    tokens.made_for = (batch, k.shape[2])
+    return tokens
 
 
 def swarm_append_tokens(ctx, inputs: swarm_inputs, tokens: swarm_new_tokens, kv_pool: torch.Tensor,
                         ksum: Optional[torch.Tensor], ctx_len_out: torch.Tensor, stream=None) -> None:
     """Writes the new tokens behind each request's, updates the summaries of the pages reached (ksum may be None) and writes
     the new lengths (ctx_len_out may be the tensor that inputs.ctx_len points to)."""
-    rc = load_library().swarm_append_tokens(ctx, ctypes.byref(inputs), ctypes.byref(tokens), _ptr(kv_pool, "kv_pool"),
-                                            _ptr(ksum, "ksum"), _ptr(ctx_len_out, "ctx_len_out"), _stream(stream))
+    if type(ctx) is not swarm_ctx:
+        ctx = _bare(ctx)
+    if tokens.made_for != ctx.made_for_tokens:
+        _other_ctx("new tokens", tokens.made_for, ctx.made_for_tokens)
+    rc = load_library().append_tokens(ctx, inputs, tokens, _holds(kv_pool, "kv_pool", _BF16, ctx.pool_elems),
+                                      None if ksum is None else _holds(ksum, "ksum", _BF16, ctx.sum_elems),
+                                      _holds(ctx_len_out, "ctx_len_out", _I32, ctx.batch), _raw_stream(stream))
     if rc != OK:
         _check(rc, "swarm_append_tokens", ctx)
 
@@ -542,14 +609,23 @@ def make_page_plan(*, page_base: torch.Tensor, ctx_len: torch.Tensor, parent: to
         _expect(reserve, "reserve", torch.int32, (batch,))
     if keep is not None:
         _expect(keep, "keep", torch.uint8, (keep.numel(),))
-    return swarm_page_plan(*[_ptr(t, n) for n, t in (("page_base", page_base), ("ctx_len", ctx_len), ("parent", parent),
+    _holds(n_moves, "n_moves", _I32, 1)
+    plan = swarm_page_plan(*[_ptr(t, n) for n, t in (("page_base", page_base), ("ctx_len", ctx_len), ("parent", parent),
                                                      ("reserve", reserve), ("keep", keep), ("new_page_base", new_page_base),
                                                      ("new_ctx_len", new_ctx_len), ("src", src), ("dst", dst),
                                                      ("n_moves", n_moves))], src.numel(), 1 if in_place else 0)
+    plan.made_for, plan.n_keep = batch, None if keep is None else keep.numel()
+    return plan
 
 
 def swarm_plan_pages(ctx, plan: swarm_page_plan, stream=None) -> None:
-    rc = load_library().swarm_plan_pages(ctx, ctypes.byref(plan), _stream(stream))
+    if type(ctx) is not swarm_ctx:
+        ctx = _bare(ctx)
+    if plan.made_for != ctx.batch:
+        _other_ctx("plan", plan.made_for, ctx.batch)
+    if plan.n_keep is not None and plan.n_keep < ctx.n_pool_pages:
+        raise ValueError(f"keep must have an entry for each of the {ctx.n_pool_pages} pages of the pool, not {plan.n_keep}")
+    rc = load_library().plan_pages(ctx, plan, _raw_stream(stream))
     if rc != OK:
         _check(rc, "swarm_plan_pages", ctx)
 
@@ -565,10 +641,18 @@ def make_page_moves(*, src: torch.Tensor, dst: torch.Tensor, n_moves: torch.Tens
     for name, a, b in (("pool", from_pool, to_pool), ("ksum", from_ksum, to_ksum), ("page2cluster", from_page2cluster, to_page2cluster)):
         if a is not None and b is not None:
             _expect(b, f"to_{name}", a.dtype, a.shape)
-    return swarm_page_moves(*[_ptr(t, n) for n, t in (("src", src), ("dst", dst), ("n_moves", n_moves), ("from_pool", from_pool),
+    _holds(n_moves, "n_moves", _I32, 1)
+    tables = []
+    for name, t, dtype in (("pool", from_pool, _BF16), ("ksum", from_ksum, _BF16), ("page2cluster", from_page2cluster, _I32)):
+        if t is not None:
+            _holds(t, f"from_{name}", dtype, 0)
+        tables.append(None if t is None else t.numel())
+    moves = swarm_page_moves(*[_ptr(t, n) for n, t in (("src", src), ("dst", dst), ("n_moves", n_moves), ("from_pool", from_pool),
                                                       ("to_pool", to_pool), ("from_ksum", from_ksum), ("to_ksum", to_ksum),
                                                       ("from_page2cluster", from_page2cluster),
                                                       ("to_page2cluster", to_page2cluster))], src.numel(), 0)
+    moves.made_for = tables
+    return moves
 
 
 def swarm_move_pages_workspace_bytes(shape: swarm_shape) -> int:
@@ -579,8 +663,12 @@ def swarm_move_pages_workspace_bytes(shape: swarm_shape) -> int:
 
 
 def swarm_move_pages(ctx, moves: swarm_page_moves, workspace: torch.Tensor, stream=None) -> None:
-    rc = load_library().swarm_move_pages(ctx, ctypes.byref(moves), _ptr(workspace, "workspace"),
-                                         ctypes.c_int64(workspace.numel() * workspace.element_size()), _stream(stream))
+    if type(ctx) is not swarm_ctx:
+        ctx = _bare(ctx)
+    for name, has, needs in zip(("pool", "ksum", "page2cluster"), moves.made_for or (), (ctx.pool_elems, ctx.sum_elems, ctx.n_pool_pages)):
+        if has is not None and has < needs:
+            raise ValueError(f"{name} must hold the pool's {ctx.n_pool_pages} pages: {needs} elements, not {has}")
+    rc = load_library().move_pages(ctx, moves, _ptr(workspace, "workspace"), workspace.nbytes, _raw_stream(stream))
     if rc != OK:
         _check(rc, "swarm_move_pages", ctx)
 

@@ -1,5 +1,6 @@
 """Decoding with several continuations, as a serving program runs it: drafted trees attended and committed through a Session, beams
 selected, forked and compacted; on streams, in captured graphs, in pools beyond 32-bit offsets; and what is refused."""
+import ctypes
 import math
 
 import numpy as np
@@ -688,3 +689,69 @@ def test_nothing_is_compacted_under_a_cache_state():
     s.compact(dev([1, -1, 2]))
     assert s.status() == 0 and w.ctx_len.tolist()[1] == 0
     s.close()
+
+
+def refused(call, match):
+    with pytest.raises(ValueError, match=match):
+        call()
+
+
+def test_tensors_that_are_too_small_or_of_another_type_are_refused():
+    """What the kernels would read or write past the end of: refused by the binding, nothing is launched."""
+    c = Case(lens=[60, 40], T=2, n_draft=[2, 2], hq=4, hkv=2, S=16, seed=1, top_k=3)
+
+    def tree(tree=c.tree, sel=c.sel, n_sel=c.n_sel, out=c.out, lse=c.lse):
+        B.swarm_tree_attn(c.ctx, c.inputs, tree, sel, n_sel, c.ws, out, lse)
+
+    for kw, match in ((dict(out=c.out[:1]), "out"), (dict(out=c.out.float()), "out"), (dict(lse=c.lse[:, :1].contiguous()), "lse"),
+                      (dict(lse=c.lse.half()), "lse"), (dict(sel=c.sel[..., :2].contiguous()), "sel"), (dict(sel=c.sel.long()), "sel"),
+                      (dict(n_sel=c.n_sel[:1]), "n_sel"), (dict(n_sel=c.n_sel.long()), "n_sel")):
+        refused(lambda: tree(**kw), match)
+    one = [x[:1].contiguous() for x in (c.q, c.k, c.v, c.nd)]   # drafts of fewer requests, of fewer heads
+    refused(lambda: tree(tree=B.make_tree(q=one[0], k=one[1], v=one[2], n_draft=one[3])), "made for")
+    few = [x[:, :, :1].contiguous() for x in (c.q, c.k, c.v)]
+    refused(lambda: tree(tree=B.make_tree(q=few[0], k=c.k, v=c.v, n_draft=c.nd)), "made for")
+    refused(lambda: tree(tree=B.make_tree(q=c.q, k=few[1], v=few[2], n_draft=c.nd)), "made for")
+
+    tokens = B.make_new_tokens(k=c.k, v=c.v, n_new=c.nd)
+    ksum = torch.zeros((c.pool.shape[0], 2, 2, 128), dtype=torch.bfloat16, device=DEV)
+    lens = torch.zeros(2, dtype=torch.int32, device=DEV)
+
+    def append(tokens=tokens, pool=c.pool, ksum=ksum, lens=lens):
+        B.swarm_append_tokens(c.ctx, c.inputs, tokens, pool, ksum, lens)
+
+    for kw, match in ((dict(pool=c.pool[1:]), "kv_pool"), (dict(pool=c.pool.float()), "kv_pool"), (dict(ksum=ksum[1:]), "ksum"),
+                      (dict(ksum=ksum.float()), "ksum"), (dict(lens=lens[:1]), "ctx_len_out"), (dict(lens=lens.long()), "ctx_len_out"),
+                      (dict(tokens=B.make_new_tokens(k=one[1], v=one[2], n_new=one[3])), "made for"),
+                      (dict(tokens=B.make_new_tokens(k=few[1], v=few[2], n_new=c.nd)), "made for")):
+        refused(lambda: append(**kw), match)
+    c.pool.nan_to_num_(0)
+    before = c.pool.clone()
+    tree()
+    B.swarm_tree_attn(ctypes.c_void_p(c.ctx.value), c.inputs, c.tree, c.sel, c.n_sel, c.ws, c.out, c.lse)   # (a bare handle will do)
+    torch.cuda.synchronize()
+    assert B.swarm_device_status(c.ctx) == 0 and torch.equal(c.pool, before) and not bool(lens.any()) and not bool(ksum.any())
+    c.close()
+
+    lay = Layout([20, 40], [2, 4], 8)
+    n, keep = dev([0]), torch.ones(8, dtype=torch.uint8, device=DEV)
+    t = dict(page_base=lay.page_base, ctx_len=lay.ctx_len, parent=dev([0, 1]), new_page_base=torch.zeros_like(lay.page_base),
+             new_ctx_len=torch.zeros_like(lay.ctx_len), src=torch.zeros(8, dtype=torch.int32, device=DEV),
+             dst=torch.zeros(8, dtype=torch.int32, device=DEV), n_moves=n)
+    refused(lambda: B.make_page_plan(**{**t, "n_moves": n.long()}), "n_moves")
+    refused(lambda: B.make_page_plan(**{**t, "n_moves": n[:0]}), "n_moves")
+    refused(lambda: B.swarm_plan_pages(lay.ctx, B.make_page_plan(**t, keep=keep[:7])), "keep")
+    less = {**t, "parent": dev([0]), "page_base": lay.page_base[:2], "ctx_len": lay.ctx_len[:1], "new_page_base": t["new_page_base"][:2],
+            "new_ctx_len": t["new_ctx_len"][:1]}
+    refused(lambda: B.swarm_plan_pages(lay.ctx, B.make_page_plan(**less)), "made for")
+    pairs = dict(src=t["src"], dst=t["dst"], n_moves=n)
+    refused(lambda: B.make_page_moves(**{**pairs, "n_moves": n.long()}, from_pool=lay.pool, to_pool=lay.pool), "n_moves")
+    refused(lambda: B.make_page_moves(**pairs, from_pool=lay.pool.view(torch.int16), to_pool=lay.pool.view(torch.int16)), "from_pool")
+    wide = lay.p2c.long()
+    for kw, match in ((dict(from_pool=lay.pool[1:], to_pool=lay.pool[1:]), "pool"),
+                      (dict(from_pool=lay.pool, to_pool=lay.pool, from_ksum=lay.ksum[1:], to_ksum=lay.ksum[1:]), "ksum"),
+                      (dict(from_pool=lay.pool, to_pool=lay.pool, from_page2cluster=lay.p2c[:4], to_page2cluster=lay.p2c[:4]), "page2cluster"),
+                      (dict(from_pool=lay.pool, to_pool=lay.pool, from_page2cluster=wide, to_page2cluster=wide), "page2cluster")):
+        refused(lambda: B.swarm_move_pages(lay.ctx, B.make_page_moves(**pairs, **kw), lay.ws), match)
+    assert B.swarm_device_status(lay.ctx) == 0
+    close(lay.ctx)
