@@ -518,7 +518,8 @@ int32_t swarm_plan_pages(swarm_ctx* ctx, const swarm_page_plan* plan, void* stre
  * one call at a time; < 0: minus an error code.  SWARM_ERR_UNSUPPORTED: n_pool_pages or max_moves >= 2^30, or more than about 2^31
  * blocks of 32 KB in max_moves pages.
  * page2cluster holds ids local to a request and is moved as it is: where requests change places, cluster_base and the
- * tables it points into are the caller's to permute, those of an attached cache state (swarm_set_cache) among them.  With a tail stream, swarm_tail_join comes before moves inside the pool. */
+ * tables it points into are the caller's to permute, those of an attached cache state (swarm_set_cache) among them.  With a
+ * tail stream, swarm_tail_join comes before moves inside the pool. */
 int64_t swarm_move_pages_workspace_bytes(const swarm_shape* shape);
 int32_t swarm_move_pages(swarm_ctx* ctx, const swarm_page_moves* moves, void* workspace, int64_t workspace_bytes, void* stream);
 
@@ -529,7 +530,8 @@ int32_t swarm_move_pages(swarm_ctx* ctx, const swarm_page_moves* moves, void* wo
  *   token[b][i] = v.
  * Continuations of -inf or NaN are never chosen; where fewer than n_keep are left, new_score = -inf, parent = token = -1.
  * Logits must be below +inf.  logits: SWARM_DTYPE_*, row (b, k) starts (b * n_beams + k) * row_stride elements behind the
- * first (row_stride >= vocab).  score f32 [batch][n_beams]; outputs [batch][n_keep]; 1 <= n_keep <= 64.
+ * first (row_stride >= vocab); aligned to their own size only (the logits of a last token are a slice).  score f32
+ * [batch][n_beams]; outputs [batch][n_keep]; 1 <= n_keep <= 64.
  * workspace: swarm_beam_select_workspace_bytes bytes of device memory (contents irrelevant), used by one call at a time;
  * < 0: minus an error code.  SWARM_ERR_UNSUPPORTED: vocab >= 2^30, n_beams * vocab >= 2^31, or n_beams * n_keep^2
  * beyond about 2.9 million. */

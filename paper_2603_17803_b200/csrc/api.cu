@@ -1000,7 +1000,9 @@ int32_t swarm_beam_select(const void* logits, int32_t dtype, int64_t row_stride,
                           int32_t vocab, int32_t n_keep, void* workspace, int64_t workspace_bytes, float* new_score,
                           int32_t* parent, int32_t* token, void* stream) {
   SWARM_RANGE("swarm_beam_select");
-  if (bad(logits) || dtype < SWARM_DTYPE_F32 || dtype > SWARM_DTYPE_F16 || row_stride < vocab || bad(score) || bad(workspace) ||
+  const uintptr_t element = dtype == SWARM_DTYPE_F32 ? 4u : 2u;   // (rows start anywhere in a 16-byte line, the first one too)
+  if (logits == nullptr || (reinterpret_cast<uintptr_t>(logits) & (element - 1u)) || dtype < SWARM_DTYPE_F32 || dtype > SWARM_DTYPE_F16 ||
+      row_stride < vocab || bad(score) || bad(workspace) ||
       bad(new_score) || bad(parent) || bad(token))
     return SWARM_ERR_INVALID_ARG;
   const int32_t rc = check_beams(batch, n_beams, vocab, n_keep);

@@ -4,6 +4,7 @@ The values of a selection are compared with score + logit - log sum exp: every e
 relative, a chunk's sum adds at most 48 roundings of 2^-24: 2^-18 in all, plus the rounding of the result to fp32 (2^-24 of
 its size).  The order is compared exactly wherever neighbours differ by more than twice that, or belong to one beam (where it is
 the order of the logits, ties to the lower token)."""
+import ctypes
 import math
 
 import pytest
@@ -223,3 +224,26 @@ def test_blocks_of_nan_in_rising_rows(dtype):
         x[:, :, lo: lo + n] = math.nan
     for keep, below in ((5, 0), (33, 60), (5, 60)):
         check((x - below).to(dtype), -torch.rand((330, 2), generator=gen, device=DEV), keep)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("V", [50257, 8193, 37])
+def test_the_logits_of_the_last_token(V, dtype):
+    """A slice of a model's output: its first row starts anywhere in a 16-byte line.  What stands around it is +inf and NaN."""
+    gen = torch.Generator(device=DEV).manual_seed(V)
+    for tokens in (2, 3, 4, 5):
+        whole = torch.full((2, 3, tokens, V), math.inf, device=DEV, dtype=dtype)
+        whole[:, :, : tokens - 2] = math.nan
+        whole[:, :, -1] = (torch.randn((2, 3, V), generator=gen, device=DEV) * 3).to(dtype)
+        logits = whole[:, :, -1]
+        score = -torch.rand((2, 3), generator=gen, device=DEV)
+        check(logits, score, 9)
+        for a, b in zip(select(logits, score, 9), select(logits.contiguous(), score, 9)):
+            assert torch.equal(a, b)
+    rows = torch.zeros(4 * V + 64, device=DEV)
+    out = torch.zeros((1, 1), device=DEV)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    for off in (1, 2, 3):                                        # not a whole number of elements
+        assert B.load_library().swarm_beam_select(
+            ctypes.c_void_p(rows.data_ptr() + off), 0, ctypes.c_int64(V), ctypes.c_void_p(out.data_ptr()), 1, 1, V, 1, ctypes.c_void_p(ws.data_ptr()),
+            ctypes.c_int64(ws.numel()), *[ctypes.c_void_p(out.data_ptr())] * 3, ctypes.c_void_p(0)) == B.ERR_INVALID_ARG
