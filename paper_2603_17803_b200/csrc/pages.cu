@@ -227,9 +227,12 @@ move_setup_kernel(const Geometry geo, const MoveCall c, const MoveShape m, const
   each([&](int i, int src, int dst) {
     if (src < 0) return;
     const int order = order_of(i, n, src, dst, m.in_place);
+    if (m.in_place && src == dst) {                          // stays where it is: no item below looks at it unless some pair moves down
+      if (atomicMin(t.writer + dst, order) != 0x7FFFFFFF) atomicOr(status, SWARM_DEV_BAD_PAGE);
+      return;
+    }
     atomicMin(t.writer + dst, order);
     if (!m.in_place) { ++down; return; }
-    if (src == dst) return;                                  // stays where it is (and is overwritten by nobody else, or that is found)
     atomicMax(t.reader + src, order + 1);
     atomicAdd(t.pending + src, m.items);
     if (dst > src) ++up; else ++down;

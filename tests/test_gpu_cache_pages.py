@@ -406,3 +406,16 @@ def test_append_stops_at_the_pages_that_a_step_can_use(in_place):
     assert same(c["pool"][:4], c["want"][0][:4]) and torch.equal(c["ksum"][:4].float(), c["want"][1][:4].float())
     assert same(c["pool"][4:], before[4:]) and same(c["ksum"][4:], sums[4:])
     close(ctx)
+
+
+@pytest.mark.parametrize("pairs,done", [
+    ([(9, 9), (9, 9)], [(9, 9)]), ([(9, 9), (3, 4), (9, 9)], [(9, 9), (3, 4)]), ([(9, 9), (9, 9), (5, 2)], [(9, 9), (5, 2)]),
+    ([(9, 9), (8, 8), (3, 4)], [(9, 9), (8, 8), (3, 4)])])
+def test_a_page_that_stays_twice_is_found(pairs, done):
+    """A second pair with the same destination is one, whatever else moves."""
+    lay = Layout([16], [1], 40, hkv=2)
+    want = lay.expect(done)
+    lay.moves(src=[p[0] for p in pairs], dst=[p[1] for p in pairs])
+    assert lay.matches(want)
+    assert B.swarm_device_status(lay.ctx) == (0 if len(done) == len(pairs) else B.DEV_BAD_PAGE)
+    close(lay.ctx)
