@@ -525,7 +525,8 @@ int32_t swarm_move_pages(swarm_ctx* ctx, const swarm_page_moves* moves, void* wo
 
 /* Beam search's selection (no ctx).  Of all continuations of a prompt by a token of one of its beams the n_keep with the largest
  *   score[b][k] + logits[b][k][v] - log sum_v' exp(logits[b][k][v'])
- * in descending order, ties to the lowest k * vocab + v (compared in 64 bits):
+ * in descending order, ties to the lowest k * vocab + v.  Sums are compared in 64 bits; the log sum exp in them is one of fp32
+ * sums, so that continuations of different beams closer than 2^-18 may come in either order (equal rows have equal ones).
  *   new_score[b][i] that sum, parent[b][i] = b * n_beams + k (the row of the beam it continues, as swarm_plan_pages takes it),
  *   token[b][i] = v.
  * Continuations of -inf or NaN are never chosen; where fewer than n_keep are left, new_score = -inf, parent = token = -1.

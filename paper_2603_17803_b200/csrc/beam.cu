@@ -547,8 +547,8 @@ struct Cut {
 Cut cut_of(long long rows, int vocab, int dtype) {
   Cut c;
   auto chunks = [&](int per) { return (vocab + kBeamThreads * per - 1) / (kBeamThreads * per); };
-  c.per = dtype == SWARM_DTYPE_F32 || rows * chunks(32) < 148 ? 16 : 32;
-  const long long at_once = 148 * (c.per == 32 ? 3 : 4);
+  c.per = dtype == SWARM_DTYPE_F32 || rows * chunks(32) < kSms ? 16 : 32;
+  const long long at_once = kSms * (c.per == 32 ? 3 : 4);
   const int most = (int)std::max<long long>(1, std::min<long long>(chunks(c.per), at_once / rows));
   c.span = (chunks(c.per) + most - 1) / most;
   c.stretches = (chunks(c.per) + c.span - 1) / c.span;

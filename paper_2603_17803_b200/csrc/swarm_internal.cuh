@@ -143,6 +143,7 @@ struct Geometry {   // plain copy of the shape in kernel-friendly form
 // ---- one-time per-device kernel attribute set-up (dynamic shared-memory limits) ---------------
 cudaError_t configure_score();
 int sm_count();         // SMs of the device current at configure_score() (148 on B200)
+constexpr int kSms = 148;   // of a B200: where the size of a workspace depends on them, which has to be the same before a ctx exists
 cudaError_t configure_topk();
 enum SelectKind { kSelectRegs, kSelectSmem512, kSelectSmem1024, kSelectGeneric };
 SelectKind select_kind(int Pmax, long long lists);   // the selection kernel launched for `lists` lists of up to Pmax pages

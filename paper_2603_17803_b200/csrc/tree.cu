@@ -20,8 +20,8 @@
 // are; a unit that is cut leaves partial (m, l, O) per CTA, joined by a second kernel with a lane per row.
 //
 // What bounds it.  Up to 128 rows, HBM: 16 tokens x 4 heads over 128K tokens (537 MB) take 90 us, 6.0 TB/s.  More rows, the chain of a
-// tile: product, scores to registers, maximum, exponentials, P back, product.  Two streams overlap theirs, and the tensor cores work
-// 55 % of the time: 64 tokens x 8 heads over 256K tokens (550 GFLOP) take 495 us, 1.11 PFLOP/s at full clocks (570 us where the power
+// tile: product, scores to registers, maximum, exponentials, P back, product.  Two streams overlap theirs, and the tensor pipe is active in
+// 48 % of the cycles (64K tokens): 64 tokens x 8 heads over 256K tokens (550 GFLOP) take 495 us, 1.11 PFLOP/s at full clocks (570-590 us where the power
 // limit holds the clock at 1.45 GHz).  Leaving out half of the scores' products gained 7 % there, of O's products 3 %, the exponentials
 // 8 %: no unit by itself.  Selected pages: 8 x 16 tokens over 256 pages a head (338 MB) take 76 us, of which 6 build the lists; the
 // copies are of 2 KB (K) and 4 KB (V), with larger ones it would be 71.  A short prompt (777 tokens) takes 10 us: two launches, a
@@ -45,7 +45,7 @@ constexpr int kThreads = (kSoftWarps + 4) * 32;
 constexpr int kLoadWarp = kSoftWarps, kMmaWarp = kSoftWarps + 1, kQueryWarp = kSoftWarps + 2,
               kListWarp = kSoftWarps + 3;
 constexpr int kSegs = 32;                                  // segments of a CTA listed at a time
-constexpr int kMaxTreeCtas = 148;
+constexpr int kMaxTreeCtas = kSms;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr unsigned kWaitLimit = 1u << 22;                  // polls of a try_wait that itself blocks briefly

@@ -1,7 +1,7 @@
 """Convenience wrapper: owns a swarm ctx, its workspace and output tensors for one set of device inputs.
 
-Allocation and marshalling only (torch supplies device memory and streams); all computing is done by
-the library's kernels through ``binding``.
+Allocation and marshalling (torch supplies device memory and streams); computing is done by the library's kernels through
+``binding``, but for the cluster tables of a compaction, a few small tensors that torch permutes.
 """
 from __future__ import annotations
 
