@@ -488,7 +488,8 @@ int32_t swarm_tree_attn(swarm_ctx* ctx, const swarm_inputs* inputs, const swarm_
  * the accepted path of a drafted tree (new->path; a token may be named twice) and for prompts.
  * A request whose new length does not fit the pages it owns or max_pages_per_req (no step could use it then), whose pages lie
  * outside the pool, or with n_new out of range sets SWARM_DEV_BAD_LENGTH and is left as it was.  A path entry outside 0..T-1 sets SWARM_DEV_BAD_TOKEN; its rows are written as zeros.
- * page2cluster entries of pages that are written to for the first time are the caller's.  With a tail stream, swarm_tail_join
+ * page2cluster entries of pages that are written to for the first time are the caller's, and so is a medoid index, whose
+ * summaries are copies (swarm_build_medoid_index).  With a tail stream, swarm_tail_join
  * comes first; with the index prefetch on, at least one operation between this call and the step.
  * Reads inputs->page_base, ctx_len.  kv_pool as in swarm_inputs, ksum bf16 [n_pool_pages][Hkv][2][d] or NULL. */
 int32_t swarm_append_tokens(swarm_ctx* ctx, const swarm_inputs* inputs, const swarm_new_tokens* tokens, void* kv_pool,

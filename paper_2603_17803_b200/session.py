@@ -239,15 +239,16 @@ class Session:
         """swarm_append_tokens into the session's pool: the tokens (k / v [B, T, Hkv, d], all or the accepted ``path``), the
         summaries of the pages they reach and the workload's context lengths, all in place.  The page2cluster entries of
         pages that are reached for the first time are the caller's.  A request that would pass the pages it owns or the session's
-        max_pages_per_req stays as it was and shows in status()."""
+        max_pages_per_req stays as it was and shows in status().  With a medoid index the medoids' summaries are copied anew; pages
+        that are reached for the first time are in its lists once page2cluster has them and enable_medoid_index() is called again."""
         cfg = self.cfg
-        if hasattr(self, "medoid_index"):
-            raise ValueError("the medoid index holds summaries and lists of the pages there were: append before enable_medoid_index()")
         self._about_to_write(stream)
         if k.dim() != 4 or tuple(k.shape) != (cfg.batch, k.shape[1], cfg.n_kv_heads, cfg.head_dim):
             raise ValueError(f"k must have shape {(cfg.batch, 'T', cfg.n_kv_heads, cfg.head_dim)}, not {tuple(k.shape)}")
         tokens = B.make_new_tokens(k=k, v=v, n_new=n_new, path=path)
         B.swarm_append_tokens(self.ctx, self.inputs, tokens, self.w.kv_pool, self.ksum, self.w.ctx_len, stream)
+        if hasattr(self, "medoid_index"):
+            B.swarm_build_medoid_index(self.ctx, self.inputs, self.medoid_page, self.medoid_ksum, self.cluster_ctx_len, stream)
 
     def compact(self, parent, reserve=None, keep=None, stream=None) -> None:
         """swarm_plan_pages and swarm_move_pages inside the session's pool: new request j continues old request parent[j]

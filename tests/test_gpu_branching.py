@@ -656,20 +656,46 @@ def test_a_request_grows_past_its_configured_length(S):
         fresh.close()
 
 
-def test_nothing_is_appended_under_a_medoid_index():
-    """The index copies the summaries of the medoids' pages and lists the clusters' pages: both would be stale."""
-    cfg = small(ctx_len=16 * 60 + 7)
+@pytest.mark.parametrize("in_stream", [False, True])
+def test_the_medoid_index_follows_an_append(in_stream):
+    """The index copies the summaries of the medoids' pages: one that gains tokens bounds them too, and the medoid step is that of a
+    new session over the same tokens.  Here the medoid of the last page's cluster is that page."""
+    cfg = small(ctx_len=16 * 60 + 3, top_k=24)
     w = W.generate(cfg, seed=14, device=DEV)
     s = Session(w)
-    kv = torch.zeros((3, 1, cfg.n_kv_heads, 128), dtype=torch.bfloat16, device=DEV)
-    s.append(kv, kv, dev([1, 1, 1]))
-    s.enable_medoid_index(4)
-    pool, ksum, lens = w.kv_pool.clone(), s.ksum.clone(), w.ctx_len.clone()
-    with pytest.raises(ValueError, match="medoid"):
-        s.append(kv, kv, dev([1, 1, 1]))
-    assert s.status() == 0
-    assert same(w.kv_pool, pool) and same(s.ksum, ksum) and torch.equal(w.ctx_len, lens)
+    s.enable_medoid_index(4, keep_scores=True)
+    lens, base, cbase = w.ctx_len.tolist(), w.page_base.tolist(), w.cluster_base.tolist()
+    rows = []
+    for b in range(3):
+        last = -(-lens[b] // 16) - 1
+        rows.append(cbase[b] + int(w.page2cluster[base[b] + last]))
+        s.medoid_page[rows[-1]] = last
+    B.swarm_build_medoid_index(s.ctx, s.inputs, s.medoid_page, s.medoid_ksum, s.cluster_ctx_len)
+    before = s.medoid_ksum.clone()
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    k, v = (torch.randn((3, 5, cfg.n_kv_heads, 128), generator=gen, device=DEV).to(torch.bfloat16) * 8 for _ in range(2))
+    more = [min(5, 16 - lens[b] % 16) if lens[b] % 16 else 0 for b in range(3)]
+    assert max(more) > 0
+    n_new = dev(more)
+    stream = torch.cuda.Stream() if in_stream else None
+    torch.cuda.synchronize()
+    s.append(k, v, n_new, stream=stream)
+    torch.cuda.synchronize()
+    fresh = Session(w)
+    fresh.enable_medoid_index(4, keep_scores=True)
+    fresh.medoid_page.copy_(s.medoid_page)
+    B.swarm_build_medoid_index(fresh.ctx, fresh.inputs, fresh.medoid_page, fresh.medoid_ksum, fresh.cluster_ctx_len)
+    for x in (s, fresh):
+        x.step_medoid()
+    torch.cuda.synchronize()
+    assert same(s.medoid_ksum, fresh.medoid_ksum) and torch.equal(s.cluster_ctx_len[:3], fresh.cluster_ctx_len[:3])
+    for b in range(3):                                          # (the large new keys widen the bounds)
+        assert same(s.medoid_ksum[rows[b]], before[rows[b]]) == (more[b] == 0)
+    for a, b in ((s.cluster_scores, fresh.cluster_scores), (s.sel_clusters, fresh.sel_clusters), (s.o.out, fresh.o.out), (s.o.lse, fresh.o.lse)):
+        assert same(a, b)
+    assert s.status() == 0 and fresh.status() == 0
     s.close()
+    fresh.close()
 
 
 def test_nothing_is_compacted_under_a_cache_state():
