@@ -20,12 +20,12 @@
 // are; a unit that is cut leaves partial (m, l, O) per CTA, joined by a second kernel with a lane per row.
 //
 // What bounds it.  Up to 128 rows, HBM: 16 tokens x 4 heads over 128K tokens (537 MB) take 90 us, 6.0 TB/s.  More rows, the chain of a
-// tile: product, scores to registers, maximum, exponentials, P back, product.  Two streams overlap theirs, and the tensor pipe is active in
-// 48 % of the cycles (64K tokens): 64 tokens x 8 heads over 256K tokens (550 GFLOP) take 495 us, 1.11 PFLOP/s at full clocks (570-590 us where the power
-// limit holds the clock at 1.45 GHz).  Leaving out half of the scores' products gained 7 % there, of O's products 3 %, the exponentials
-// 8 %: no unit by itself.  Selected pages: 8 x 16 tokens over 256 pages a head (338 MB) take 76 us, of which 6 build the lists; the
-// copies are of 2 KB (K) and 4 KB (V), with larger ones it would be 71.  A short prompt (777 tokens) takes 10 us: two launches, a
-// first tile from DRAM, the chain of two tiles, and the joining.
+// tile: product, scores to registers, maximum, exponentials, P back, product.  Two streams overlap theirs, and the tensor pipe is
+// active in 48 % of the cycles (64K tokens): 64 tokens x 8 heads over 256K tokens (550 GFLOP) take 495 us, 1.11 PFLOP/s at full
+// clocks (570-590 us where the power limit holds the clock at 1.45 GHz).  Leaving out half of the scores' products gained 7 % there,
+// of O's products 3 %, the exponentials 8 %: no unit by itself.  Selected pages: 8 x 16 tokens over 256 pages a head (338 MB) take
+// 76 us, of which 6 build the lists; the copies are of 2 KB (K) and 4 KB (V), with larger ones it would be 71.  A short prompt (777
+// tokens) takes 10 us: two launches, a first tile from DRAM, the chain of two tiles, and the joining.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
