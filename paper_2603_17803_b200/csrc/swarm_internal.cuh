@@ -422,8 +422,8 @@ __device__ __forceinline__ uint4 ldg_nc_v4(const void* p) {
   return r;
 }
 
-// (right up to the largest length: ctx_len + S - 1 would not be)
-__device__ __forceinline__ int pages_of(int ctx_len, int S) { return ctx_len > 0 ? (ctx_len - 1) / S + 1 : 0; }
+// ceil(ctx_len / S), S = 16 or 32, right up to the largest length (where ctx_len + S - 1 would overflow); <= 0 for lengths below 1
+__device__ __forceinline__ int pages_of(int ctx_len, int S) { return (ctx_len >> (4 + (S >> 5))) + ((ctx_len & (S - 1)) != 0); }
 
 // Programmatic dependent launch: a kernel launched with the programmatic-serialization attribute may
 // start while its predecessor in the stream is still running; it must call pdl_wait() before it
