@@ -466,8 +466,10 @@ def _step_host_fn():
 _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 
 
-def _holds(t: torch.Tensor, name: str, dtype, n: int) -> int:
-    """Address of a CUDA tensor of n elements of the type or more, in whatever shape."""
+def _holds(t: Optional[torch.Tensor], name: str, dtype, n: int) -> Optional[int]:
+    """Address of a CUDA tensor of n elements of the type or more, in whatever shape (None stays None, for the library to judge)."""
+    if t is None:
+        return None
     if t.dtype is dtype and t.numel() >= n and t.is_cuda and t.is_contiguous():
         return t.data_ptr()
     if t.is_cuda and t.is_contiguous():
@@ -587,7 +589,7 @@ def swarm_append_tokens(ctx, inputs: swarm_inputs, tokens: swarm_new_tokens, kv_
     if tokens.made_for != ctx.made_for_tokens:
         _other_ctx("new tokens", tokens.made_for, ctx.made_for_tokens)
     rc = load_library().append_tokens(ctx, inputs, tokens, _holds(kv_pool, "kv_pool", _BF16, ctx.pool_elems),
-                                      None if ksum is None else _holds(ksum, "ksum", _BF16, ctx.sum_elems),
+                                      _holds(ksum, "ksum", _BF16, ctx.sum_elems),
                                       _holds(ctx_len_out, "ctx_len_out", _I32, ctx.batch), _raw_stream(stream))
     if rc != OK:
         _check(rc, "swarm_append_tokens", ctx)

@@ -733,6 +733,11 @@ def test_tensors_that_are_too_small_or_of_another_type_are_refused():
                       (dict(lse=c.lse.half()), "lse"), (dict(sel=c.sel[..., :2].contiguous()), "sel"), (dict(sel=c.sel.long()), "sel"),
                       (dict(n_sel=c.n_sel[:1]), "n_sel"), (dict(n_sel=c.n_sel.long()), "n_sel")):
         refused(lambda: tree(**kw), match)
+    for call in (lambda: tree(out=None), lambda: tree(lse=None), lambda: B.swarm_append_tokens(
+            c.ctx, c.inputs, B.make_new_tokens(k=c.k, v=c.v, n_new=c.nd), None, None, c.nd.clone())):
+        with pytest.raises(B.SwarmError) as e:                  # what is not there is the library's to refuse
+            call()
+        assert e.value.code == B.ERR_INVALID_ARG
     one = [x[:1].contiguous() for x in (c.q, c.k, c.v, c.nd)]   # drafts of fewer requests, of fewer heads
     refused(lambda: tree(tree=B.make_tree(q=one[0], k=one[1], v=one[2], n_draft=one[3])), "made for")
     few = [x[:, :, :1].contiguous() for x in (c.q, c.k, c.v)]
