@@ -467,7 +467,7 @@ _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 
 
 def _holds(t: Optional[torch.Tensor], name: str, dtype, n: int) -> Optional[int]:
-    """Address of a CUDA tensor of n elements of the type or more, in whatever shape (None stays None, for the library to judge)."""
+    """Address of a CUDA tensor of n elements of the type or more, in whatever shape (None stays None: the library refuses it where it is needed)."""
     if t is None:
         return None
     if t.dtype is dtype and t.numel() >= n and t.is_cuda and t.is_contiguous():
